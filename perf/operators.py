@@ -296,7 +296,7 @@ def run(s):
                 B.uq_mx_dequantize(q, s["values"])
             if along_cols:
                 B.uq_mx_dequantize(qt, s["values_t"])
-            return [s["values"]] * along_rows + [s["values_t"]] * along_cols
+            return [s[name] for name in ("values", "values_t") if name in s]
         h = _draws(s["seed"], r, c, s["x"].device) if bits else None
         out = [_plain_quantize(s["x"], h).to(dt)] if along_rows else []
         if along_cols:
