@@ -450,6 +450,68 @@ int uq_randk_scatter(int64_t d, int64_t K, const int64_t *sel, const float *vals
 int uq_randk_update(int64_t d, int64_t K, const int64_t *sel, const float *vals, float *theta,
                     float lr, uint32_t *status, void *stream);
 
+/*
+ * The operators of a layer whose weight gradients go into a worker's row of g: microscaled 4-bit quantization and
+ * product, and layer norm.  A matrix is row-major with `ld` elements between its rows (ld >= columns) and any
+ * alignment of its element type; rows and columns are at most 2^30.  Where nothing else is said, an output must not
+ * overlap an input.
+ *
+ * Microscaled matrix: rows x cols values, 4-bit E2M1 numbers (0, 0.5, 1, 1.5, 2, 3, 4, 6; codes 0..7, +8 for the sign)
+ * with one power of two 2^e (E8M0 byte e + 127; 255 is NaN) per block of 32 values of a row.
+ *   codes   row r at codes + r*code_stride bytes, two values per byte, the even column in the low half; 16-byte aligned,
+ *           code_stride a multiple of 16 and >= 16*ceil(cols/32); the last block's missing values are zeros
+ *   scales  uq_mx_scale_bytes(rows, cols) bytes, 16-byte aligned: tiles of 128 rows x 4 blocks (512 bytes), the tiles of
+ *           128 rows one after the other; row r and block b of a tile at byte (r%32)*16 + (r/32)*4 + b.  Blocks of a row
+ *           beyond its last are written as 0, scales of rows beyond the last are unspecified.
+ */
+typedef struct uq_mx {
+    int64_t rows, cols;
+    int64_t code_stride;    /* bytes */
+    uint8_t *codes;
+    uint8_t *scales;
+} uq_mx;
+size_t uq_mx_scale_bytes(int64_t rows, int64_t cols);
+
+/*
+ * uq_mx_quantize — x to microscaled 4-bit values, from one read of x: q with blocks along x's rows, qt = the transposed
+ * matrix (cols x rows) with blocks along x's columns; either may be NULL.
+ *   e is the smallest integer >= -127 with max|x| <= 6 * 2^e in the block, so no value saturates.
+ *   rng_bits = 0:  x / 2^e to the nearest E2M1 number, ties to the even code
+ *   rng_bits = 16: stochastic, E Q(x) = x up to 2^-17 of a step: with the neighbours' distance u and p = (|x|/2^e - lower) / u,
+ *                  up iff h < rint(p * 2^16).  h: Philox4x32-10, key = seed, counter = (col/8, row, 0, 0x4D584634), word
+ *                  (col%8)/2, even columns the low half; one draw per value, the same in both orientations.
+ *   status: UQ_STATUS_NONFINITE; a block with a NaN or an infinity gets the scale NaN and codes 0.
+ * uq_mx_dequantize — the values, exact in binary32 and in bf16 (a block with max|x| > 1.5 * 2^127 may give infinities).
+ * uq_mx_product — out[i][j] = sum over k of a[i][k] * b[j][k] (+ add[i][j], if add is not NULL; it may be out itself with
+ *   the same ld), binary32 sums rounded once to `dtype`, the type of add and out.  a, b: the same cols >= 1.
+ *   status: UQ_STATUS_TIMEOUT if a bounded wait inside the kernel ran out (out is then not complete).
+ */
+int uq_mx_quantize(const void *x, int64_t rows, int64_t cols, int64_t ld, int dtype, uint64_t seed, int rng_bits,
+                   const uq_mx *q, const uq_mx *qt, uint32_t *status, void *stream);
+int uq_mx_dequantize(const uq_mx *q, void *out, int64_t ld, int dtype, void *stream);
+int uq_mx_product(const uq_mx *a, const uq_mx *b, const void *add, int64_t add_ld, void *out, int64_t ld, int dtype,
+                  uint32_t *status, void *stream);
+
+/*
+ * uq_layer_norm — per row: mean = sum x / cols, var = sum (x - mean)^2 / cols, rstd = 1 / sqrt(var + eps),
+ *   y = (x - mean) * rstd * gamma + beta.  dtype is the type of x and y; gamma, beta, mean, rstd are binary32; gamma and
+ *   beta may be NULL (1 and 0), and any of y, mean, rstd, q.  q receives y (rounded to dtype) quantized to the nearest, as
+ *   uq_mx_quantize would write it.  status (only with q): UQ_STATUS_NONFINITE.  cols >= 1.
+ * uq_layer_norm_backward — with xh = (x - mean) * rstd and t = dy * gamma:
+ *   dx = rstd * (t - sum t / cols - xh * sum (t * xh) / cols), dgamma[c] = sum over rows of dy * xh, dbeta[c] = sum over
+ *   rows of dy, binary32 sums in an order fixed by the sizes; dgamma and dbeta (grad_dtype) may lie in a worker's row of g.
+ *   dx, dgamma, dbeta may each be NULL.  No rows: dgamma and dbeta are 0.
+ *   workspace: uq_layer_norm_workspace_bytes(rows, cols) bytes of scratch, 16-byte aligned; calls that may overlap need
+ *   one each.
+ * Errors of all: UQ_ERR_BAD_ARG, UQ_ERR_UNSUPPORTED (more than 2^31 - 1 tiles of 64 x 64), UQ_ERR_WORKSPACE, UQ_ERR_CUDA.
+ */
+int uq_layer_norm(const void *x, int64_t rows, int64_t cols, int64_t ld, int dtype, const float *gamma, const float *beta,
+                  float eps, void *y, int64_t y_ld, float *mean, float *rstd, const uq_mx *q, uint32_t *status, void *stream);
+size_t uq_layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+int uq_layer_norm_backward(const void *dy, int64_t dy_ld, const void *x, int64_t x_ld, int64_t rows, int64_t cols, int dtype,
+                           const float *gamma, const float *mean, const float *rstd, void *dx, int64_t dx_ld, void *dgamma,
+                           void *dbeta, int grad_dtype, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,6 +30,8 @@ EXPORTS = (
     "uq_agree_scale", "uq_agree_scale_static", "uq_encode_single", "uq_select_scale_multi", "uq_encode_multi",
     "uq_aggregate", "uq_decode", "uq_decode_update", "uq_randk_gather", "uq_randk_scatter", "uq_randk_update", "uq_index_min", "uq_decode_rows", "uq_select_encode_multi", "uq_encode_decode", "uq_select_encode_decode_multi", "uq_step",
     "uq_step_small", "uq_step_run",
+    "uq_mx_quantize", "uq_mx_dequantize", "uq_mx_product", "uq_layer_norm", "uq_layer_norm_backward", "uq_mx_scale_bytes",
+    "uq_layer_norm_workspace_bytes",
 )
 
 
@@ -53,6 +55,16 @@ class uq_step_plan(C.Structure):
                 + [("scales", C.c_int32 * 16)]
                 + [(n, C.c_void_p) for n in ("W", "idx", "lev", "out", "S_opt", "status", "workspace")]
                 + [("workspace_bytes", C.c_size_t)])
+
+
+class uq_mx(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64),
+        ("cols", C.c_int64),
+        ("code_stride", C.c_int64),
+        ("codes", C.c_void_p),
+        ("scales", C.c_void_p),
+    ]
 
 
 class UqError(RuntimeError):
@@ -110,8 +122,17 @@ def lib() -> C.CDLL:
         L.uq_randk_gather.argtypes = [LP, P, I64, U64, P, P, I64, P, P]
         L.uq_randk_scatter.argtypes = [I64, I64, P, P, P, P, P]
         L.uq_randk_update.argtypes = [I64, I64, P, P, P, F, P, P]
+        MP = C.POINTER(uq_mx)
+        L.uq_mx_quantize.argtypes = [P, I64, I64, I64, I, U64, I, MP, MP, P, P]
+        L.uq_mx_dequantize.argtypes = [MP, P, I64, I, P]
+        L.uq_mx_product.argtypes = [MP, MP, P, I64, P, I64, I, P, P]
+        L.uq_layer_norm.argtypes = [P, I64, I64, I64, I, P, P, F, P, I64, P, P, MP, P, P]
+        L.uq_layer_norm_backward.argtypes = [P, I64, P, I64, I64, I64, I, P, P, P, P, I64, P, P, I, P, SZ, P]
         for name in EXPORTS[7:]:
             getattr(L, name).restype = I
+        for name in ("uq_mx_scale_bytes", "uq_layer_norm_workspace_bytes"):
+            getattr(L, name).argtypes = [I64, I64]
+            getattr(L, name).restype = SZ
         _lib = L
     return _lib
 
@@ -480,3 +501,152 @@ def uq_step_small(layout: Layout, g: torch.Tensor, norm: int, s: int, scales: Op
         layout.ref(), _ptr(g), norm, s, arr, N, idx_bits, seed, rng_bits, fmt, _ptr(W),
         _ptr(idx) if scales is not None else None, _ptr(lev), _ptr(out), _ptr(S_opt), _ptr(status), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream()))
+
+
+# ---- a layer's operators: microscaled 4-bit matrices and layer norm ------------------------------------------------
+
+def mx_scale_bytes(rows: int, cols: int) -> int:
+    """Bytes of the scales of a rows x cols microscaled matrix (uq_mx_scale_bytes)."""
+    return -(-rows // 128) * -(-cols // 128) * 512
+
+
+class MxMatrix:
+    """A microscaled 4-bit matrix: ``codes`` [rows, >= 16 * ceil(cols / 32)] bytes, two values each, and ``scales``, one
+    power of two per block of 32 columns, in the tiles that include/uq.h describes.  Buffers that are not given are
+    allocated (scales zeroed) on the current device."""
+
+    def __init__(self, rows: int, cols: int, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                 device: str | torch.device = "cuda"):
+        if rows < 0 or cols < 0:
+            raise ValueError("uq: a microscaled matrix has no negative sizes")
+        need = 16 * -(-cols // 32)
+        if codes is None:
+            codes = torch.empty((rows, need), dtype=torch.uint8, device=device)
+        if scales is None:
+            scales = torch.zeros(mx_scale_bytes(rows, cols), dtype=torch.uint8, device=device)
+        if codes.dtype != torch.uint8 or codes.dim() != 2 or codes.shape[0] != rows or codes.shape[1] < need \
+                or (codes.shape[1] > 1 and codes.stride(1) != 1):
+            raise ValueError(f"uq: codes must be a [{rows}, >= {need}] uint8 tensor, its rows contiguous")
+        if scales.dtype != torch.uint8 or scales.dim() != 1 or not scales.is_contiguous() \
+                or scales.numel() < mx_scale_bytes(rows, cols):
+            raise ValueError(f"uq: scales must be a contiguous uint8 tensor with >= {mx_scale_bytes(rows, cols)} elements")
+        if codes.device != scales.device:
+            raise ValueError("uq: codes and scales live on different devices")
+        self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
+        stride = codes.stride(0) if rows > 1 else -(-max(need, 16) // 16) * 16
+        self.c = uq_mx(rows, cols, stride, codes.data_ptr(), scales.data_ptr())
+        self._ref = C.byref(self.c)
+        self._index = codes.get_device()
+
+    def ref(self):
+        """The C struct, for a launch on the current device."""
+        if self._index < 0:
+            raise ValueError("uq: tensors must live on a CUDA device")
+        if self._index != _current_device():
+            require_current_device(self._index, torch.cuda.current_device(), "a microscaled matrix")
+        return self._ref
+
+
+def _dtype(t: torch.Tensor, what: str) -> int:
+    if t.dtype is torch.bfloat16:
+        return UQ_BF16
+    if t.dtype is torch.float32:
+        return UQ_F32
+    raise ValueError(f"uq: {what} must be float32 or bfloat16")
+
+
+def _matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
+    """Checks a matrix whose rows are contiguous and returns the elements between its rows."""
+    if t.dtype is not dtype or t.dim() != 2:
+        raise ValueError(f"uq: {what} must be a 2-D {dtype} tensor")
+    r, c = t.shape
+    if r != rows or c != cols:
+        raise ValueError(f"uq: {what} must be [{rows}, {cols}], not [{r}, {c}]")
+    step, inner = t.stride()
+    if (inner != 1 and cols > 1) or (step < cols and rows > 1):
+        raise ValueError(f"uq: the rows of {what} must be contiguous and must not overlap")
+    return step if rows > 1 else max(step, cols)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str, dtype: torch.dtype = torch.float32) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"uq: {what} must be a contiguous 1-D {dtype} tensor with {n} elements")
+    return _ptr(t)
+
+
+def _status(t: Optional[torch.Tensor]) -> Optional[int]:
+    if t is not None and (t.dtype is not torch.int32 or t.numel() < 1):
+        raise ValueError("uq: status must be an int32 tensor")
+    return _ptr(t)
+
+
+def _shape(t: torch.Tensor, what: str):
+    if t.dim() != 2:
+        raise ValueError(f"uq: {what} must be a 2-D tensor")
+    return t.shape
+
+
+def uq_mx_quantize(x: torch.Tensor, seed: int, rng_bits: int, q: Optional[MxMatrix], qt: Optional[MxMatrix],
+                   status: Optional[torch.Tensor] = None) -> None:
+    """x [rows, cols] to microscaled 4-bit values: ``q`` with blocks along the rows, ``qt`` = the transposed matrix with
+    blocks along x's columns, or both.  rng_bits 0: to the nearest value; 16: stochastically, unbiased."""
+    (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
+    ld = _matrix(x, rows, cols, x.dtype, "x")
+    _check("uq_mx_quantize", lib().uq_mx_quantize(
+        _ptr(x), rows, cols, ld, dtype, seed & 0xFFFFFFFFFFFFFFFF, rng_bits, None if q is None else q.ref(),
+        None if qt is None else qt.ref(), _status(status), _stream()))
+
+
+def uq_mx_dequantize(q: MxMatrix, out: torch.Tensor) -> None:
+    """The values that a microscaled matrix stands for (exact in either type)."""
+    dtype, ld = _dtype(out, "out"), _matrix(out, q.rows, q.cols, out.dtype, "out")
+    _check("uq_mx_dequantize", lib().uq_mx_dequantize(q.ref(), _ptr(out), ld, dtype, _stream()))
+
+
+def uq_mx_product(a: MxMatrix, b: MxMatrix, out: torch.Tensor, add: Optional[torch.Tensor] = None,
+                  status: Optional[torch.Tensor] = None) -> None:
+    """out [a.rows, b.rows] = a b^T (+ add, which may be out itself), binary32 sums rounded once to out's type."""
+    if a.cols != b.cols:
+        raise ValueError(f"uq: the operands have {a.cols} and {b.cols} columns")
+    dtype, ld = _dtype(out, "out"), _matrix(out, a.rows, b.rows, out.dtype, "out")
+    add_ld = 0 if add is None else _matrix(add, a.rows, b.rows, out.dtype, "add")
+    _check("uq_mx_product", lib().uq_mx_product(a.ref(), b.ref(), _ptr(add), add_ld, _ptr(out), ld, dtype,
+                                                _status(status), _stream()))
+
+
+def uq_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
+                  y: Optional[torch.Tensor], mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
+                  q: Optional[MxMatrix] = None, status: Optional[torch.Tensor] = None) -> None:
+    """Layer norm over the rows of x; any of y, the statistics and the quantized y (q) may be left out."""
+    (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
+    ld = _matrix(x, rows, cols, x.dtype, "x")
+    y_ld = 0 if y is None else _matrix(y, rows, cols, x.dtype, "y")
+    _check("uq_layer_norm", lib().uq_layer_norm(
+        _ptr(x), rows, cols, ld, dtype, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, _ptr(y), y_ld,
+        _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), None if q is None else q.ref(), _status(status), _stream()))
+
+
+def uq_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().uq_layer_norm_workspace_bytes(rows, cols))
+
+
+def uq_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[torch.Tensor], mean: torch.Tensor,
+                           rstd: torch.Tensor, dx: Optional[torch.Tensor], dgamma: Optional[torch.Tensor],
+                           dbeta: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
+    """Gradients of uq_layer_norm; dgamma and dbeta (float32 or bfloat16, both the same) may be pieces of a worker's row
+    of gradients.  ``workspace``: uq_layer_norm_workspace_bytes(rows, cols) bytes."""
+    rows, cols = _shape(x, "x")
+    x_ld = _matrix(x, rows, cols, x.dtype, "x")
+    dy_ld = _matrix(dy, rows, cols, x.dtype, "dy")
+    dx_ld = 0 if dx is None else _matrix(dx, rows, cols, x.dtype, "dx")
+    grad = dgamma if dgamma is not None else dbeta
+    grad_dtype = torch.float32 if grad is None else grad.dtype
+    if not workspace.is_contiguous():
+        raise ValueError("uq: the workspace must be contiguous")
+    _check("uq_layer_norm_backward", lib().uq_layer_norm_backward(
+        _ptr(dy), dy_ld, _ptr(x), x_ld, rows, cols, _dtype(x, "x"), _vector(gamma, cols, "gamma"), _vector(mean, rows, "mean"),
+        _vector(rstd, rows, "rstd"), _ptr(dx), dx_ld, _vector(dgamma, cols, "dgamma", grad_dtype),
+        _vector(dbeta, cols, "dbeta", grad_dtype), UQ_F32 if grad is None else _dtype(grad, "dgamma and dbeta"),
+        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))

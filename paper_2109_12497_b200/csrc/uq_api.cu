@@ -1,6 +1,6 @@
 // The C ABI declared in include/uq.h: argument validation on the host, then kernel launches.
 // No allocation, no synchronization, no state besides a thread-local last CUDA error.
-#include "uq_device.cuh"
+#include "uq_mx.cuh"
 
 namespace uq {
 int64_t norm_tiles(const uq_layout &L);
@@ -32,6 +32,18 @@ size_t small_workspace_bytes();
 cudaError_t launch_small_step(const uq_layout &L, const void *g, int norm, const ScaleSet &scales, int idx_bits,
                               uint64_t seed, int rng_bits, int fmt, float *W, uint8_t *idx, void *lev, float *out,
                               int32_t *S, uint32_t *status, void *workspace, cudaStream_t st);
+cudaError_t launch_mx_quantize(const void *x, int64_t rows, int64_t cols, int64_t ld, int dtype, uint64_t seed, int rng_bits,
+                               const uq_mx &q, const uq_mx &qt, uint32_t *status, cudaStream_t st);
+cudaError_t launch_mx_dequantize(const uq_mx &q, void *out, int64_t ld, int dtype, cudaStream_t st);
+cudaError_t launch_mx_product(const uq_mx &a, const uq_mx &b, const void *add, int64_t add_ld, void *out, int64_t ld, int dtype,
+                              uint32_t *status, cudaStream_t st);
+size_t layer_norm_workspace_bytes(int64_t rows, int64_t cols);
+cudaError_t launch_layer_norm(const void *x, int64_t rows, int64_t cols, int64_t ld, int dtype, const float *gamma, const float *beta,
+                              float eps, void *y, int64_t y_ld, float *mean, float *rstd, const uq_mx &q, uint32_t *status,
+                              cudaStream_t st);
+cudaError_t launch_layer_norm_backward(const void *dy, int64_t dy_ld, const void *x, int64_t x_ld, int64_t rows, int64_t cols, int dtype,
+                                       const float *gamma, const float *mean, const float *rstd, void *dx, int64_t dx_ld, void *dgamma,
+                                       void *dbeta, int grad_dtype, void *workspace, cudaStream_t st);
 }  // namespace uq
 
 namespace {
@@ -103,6 +115,31 @@ uq::ScaleSet single_scale(int s)
     for (int k = 0; k < UQ_MAX_SCALES; ++k) set.s[k] = s;
     set.N = 1;
     return set;
+}
+
+constexpr int64_t kMaxSide = (int64_t)1 << 30;      // rows or columns of a matrix of the layer operators
+
+bool dtype_ok(int dtype) { return dtype == UQ_F32 || dtype == UQ_BF16; }
+
+bool side_ok(int64_t n) { return n >= 0 && n <= kMaxSide; }
+
+// Whether an array of `rows` rows may be used: there is one if it has elements, aligned to its element, rows not overlapping.
+bool matrix_ok(const void *p, int64_t rows, int64_t cols, int64_t ld, int dtype)
+{
+    if (rows == 0 || cols == 0) return true;
+    return p != nullptr && aligned(p, dtype == UQ_BF16 ? 2 : 4) && (rows == 1 || ld >= cols) && ld <= (int64_t)1 << 40;
+}
+
+// More tiles of 64 x 64 than a grid has blocks, or than 64-bit sizes hold.
+bool too_many(int64_t rows, int64_t cols) { return ((rows + 63) >> 6) * ((cols + 63) >> 6) > 0x7FFFFFFF; }
+
+// A microscaled matrix of that shape (what an empty one points to does not matter).
+bool mx_ok(const uq_mx *q, int64_t rows, int64_t cols)
+{
+    if (q->rows != rows || q->cols != cols || !side_ok(rows) || !side_ok(cols)) return false;
+    if (rows == 0 || cols == 0) return true;
+    return q->codes != nullptr && q->scales != nullptr && aligned(q->codes, 16) && aligned(q->scales, 16) && (q->code_stride & 15) == 0 &&
+           q->code_stride >= uq::mx_blocks(cols) * 16 && q->code_stride <= (int64_t)1 << 38;
 }
 
 }  // namespace
@@ -422,6 +459,84 @@ int uq_randk_update(int64_t d, int64_t K, const int64_t *sel, const float *vals,
                     uint32_t *status, void *stream)
 {
     return randk_scatter_common(d, K, sel, vals, theta, true, lr, status, stream);
+}
+
+size_t uq_mx_scale_bytes(int64_t rows, int64_t cols)
+{
+    if (!side_ok(rows) || !side_ok(cols)) return 0;
+    return (size_t)(uq::mx_ktiles(rows) * uq::mx_ktiles(cols)) * 512;
+}
+
+int uq_mx_quantize(const void *x, int64_t rows, int64_t cols, int64_t ld, int dtype, uint64_t seed, int rng_bits, const uq_mx *q,
+                   const uq_mx *qt, uint32_t *status, void *stream)
+{
+    if (!dtype_ok(dtype) || !side_ok(rows) || !side_ok(cols) || !matrix_ok(x, rows, cols, ld, dtype)) return UQ_ERR_BAD_ARG;
+    if ((rng_bits != 0 && rng_bits != 16) || (q == nullptr && qt == nullptr) || !aligned(status, 4)) return UQ_ERR_BAD_ARG;
+    if (q != nullptr && !mx_ok(q, rows, cols)) return UQ_ERR_BAD_ARG;
+    if (qt != nullptr && !mx_ok(qt, cols, rows)) return UQ_ERR_BAD_ARG;
+    if (too_many(rows, cols)) return UQ_ERR_UNSUPPORTED;
+    if (rows == 0 || cols == 0) return UQ_OK;
+    const uq_mx none = {};
+    return finish(uq::launch_mx_quantize(x, rows, cols, ld, dtype, seed, rng_bits, q != nullptr ? *q : none, qt != nullptr ? *qt : none,
+                                         status, (cudaStream_t)stream));
+}
+
+int uq_mx_dequantize(const uq_mx *q, void *out, int64_t ld, int dtype, void *stream)
+{
+    if (q == nullptr || !mx_ok(q, q->rows, q->cols) || !dtype_ok(dtype) || !matrix_ok(out, q->rows, q->cols, ld, dtype)) return UQ_ERR_BAD_ARG;
+    if (q->rows == 0 || q->cols == 0) return UQ_OK;
+    return finish(uq::launch_mx_dequantize(*q, out, ld, dtype, (cudaStream_t)stream));
+}
+
+int uq_mx_product(const uq_mx *a, const uq_mx *b, const void *add, int64_t add_ld, void *out, int64_t ld, int dtype, uint32_t *status,
+                  void *stream)
+{
+    if (a == nullptr || b == nullptr || a->cols != b->cols || a->cols < 1 || !dtype_ok(dtype)) return UQ_ERR_BAD_ARG;
+    if (!mx_ok(a, a->rows, a->cols) || !mx_ok(b, b->rows, b->cols)) return UQ_ERR_BAD_ARG;
+    if (!matrix_ok(out, a->rows, b->rows, ld, dtype) || !aligned(status, 4)) return UQ_ERR_BAD_ARG;
+    if (add != nullptr && !matrix_ok(add, a->rows, b->rows, add_ld, dtype)) return UQ_ERR_BAD_ARG;
+    if (too_many(a->rows, b->rows)) return UQ_ERR_UNSUPPORTED;
+    if (a->rows == 0 || b->rows == 0) return UQ_OK;
+    return finish(uq::launch_mx_product(*a, *b, add, add_ld, out, ld, dtype, status, (cudaStream_t)stream));
+}
+
+int uq_layer_norm(const void *x, int64_t rows, int64_t cols, int64_t ld, int dtype, const float *gamma, const float *beta, float eps,
+                  void *y, int64_t y_ld, float *mean, float *rstd, const uq_mx *q, uint32_t *status, void *stream)
+{
+    if (!dtype_ok(dtype) || !side_ok(rows) || !side_ok(cols) || cols < 1 || !matrix_ok(x, rows, cols, ld, dtype)) return UQ_ERR_BAD_ARG;
+    if (!(eps >= 0.0f) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(status, 4))
+        return UQ_ERR_BAD_ARG;
+    if (rows > 0 && y == nullptr && mean == nullptr && rstd == nullptr && q == nullptr) return UQ_ERR_BAD_ARG;
+    if (y != nullptr && !matrix_ok(y, rows, cols, y_ld, dtype)) return UQ_ERR_BAD_ARG;
+    if (q != nullptr && !mx_ok(q, rows, cols)) return UQ_ERR_BAD_ARG;
+    if (rows == 0) return UQ_OK;
+    const uq_mx none = {};
+    return finish(uq::launch_layer_norm(x, rows, cols, ld, dtype, gamma, beta, eps, y, y_ld, mean, rstd, q != nullptr ? *q : none, status,
+                                        (cudaStream_t)stream));
+}
+
+size_t uq_layer_norm_workspace_bytes(int64_t rows, int64_t cols)
+{
+    if (!side_ok(rows) || !side_ok(cols)) return 0;
+    return uq::layer_norm_workspace_bytes(rows, cols);
+}
+
+int uq_layer_norm_backward(const void *dy, int64_t dy_ld, const void *x, int64_t x_ld, int64_t rows, int64_t cols, int dtype,
+                           const float *gamma, const float *mean, const float *rstd, void *dx, int64_t dx_ld, void *dgamma, void *dbeta,
+                           int grad_dtype, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!dtype_ok(dtype) || !dtype_ok(grad_dtype) || !side_ok(rows) || !side_ok(cols) || cols < 1) return UQ_ERR_BAD_ARG;
+    if (!matrix_ok(dy, rows, cols, dy_ld, dtype) || !matrix_ok(x, rows, cols, x_ld, dtype)) return UQ_ERR_BAD_ARG;
+    if (rows > 0 && (mean == nullptr || rstd == nullptr)) return UQ_ERR_BAD_ARG;
+    if (!aligned(gamma, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return UQ_ERR_BAD_ARG;
+    if (dx == nullptr && dgamma == nullptr && dbeta == nullptr) return UQ_ERR_BAD_ARG;
+    if (dx != nullptr && !matrix_ok(dx, rows, cols, dx_ld, dtype)) return UQ_ERR_BAD_ARG;
+    const size_t element = grad_dtype == UQ_BF16 ? 2 : 4;
+    if (!aligned(dgamma, element) || !aligned(dbeta, element)) return UQ_ERR_BAD_ARG;
+    if (rows > 0 && (workspace == nullptr || !aligned(workspace, 16) || workspace_bytes < uq::layer_norm_workspace_bytes(rows, cols)))
+        return UQ_ERR_WORKSPACE;
+    return finish(uq::launch_layer_norm_backward(dy, dy_ld, x, x_ld, rows, cols, dtype, gamma, mean, rstd, dx, dx_ld, dgamma, dbeta,
+                                                 grad_dtype, workspace, (cudaStream_t)stream));
 }
 
 }  // extern "C"
