@@ -130,6 +130,8 @@ __device__ __forceinline__ uint2 ld_coherent64(const void *p)
 
 template <typename T> __device__ __forceinline__ void st_stream(T *p, T v) { __stcs(p, v); }
 
+__device__ __forceinline__ uint32_t smem_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
 // 16 bytes from global memory straight into shared memory; a thread's copies are complete for that thread after
 // copy_async_wait().
 __device__ __forceinline__ void copy_async16(uint32_t smem_dst, const void *gmem_src)

@@ -5,194 +5,637 @@
 //   xh = (x - mean) rstd    t = dy gamma    dx = rstd (t - sum t / n - xh sum (t xh) / n)
 //   dgamma = sum over rows of dy xh         dbeta = sum over rows of dy
 //
-// Everything is held in binary32; a result is rounded once, to the type of its array.
+// Everything is held in binary32; a result is rounded once, to the type of its array.  Both passes are bound by memory.  A CTA
+// (for up to 512 columns: a warp) takes one row after another; the next rows are on their way into a ring of three in shared
+// memory meanwhile, and a row is read from there once and kept in registers over its reductions, as are the weights and, in
+// the backward pass, the sums over the rows.  Rows may start anywhere: the ring takes whole 16-byte granules of memory, what
+// lies beside the row (but inside the matrix) included, and a row keeps its offset from 16 bytes there.  Which elements a
+// thread holds depends on that offset: eight neighbours in one 16-byte access, or eight that are 32 apart, so that a warp's
+// scalar accesses are contiguous.
 #include "uq_mx.cuh"
 
 namespace uq {
 namespace {
 
-constexpr int kLnThreads = 256;
-constexpr int kLnGrid = 296;                    // partial sums of the weight's gradient: two CTAs per SM
+constexpr int kLnThreads = 256;                            // of the kernels for any length
+constexpr int kRing = 3;                                   // rows in shared memory
+constexpr int64_t kLnRegisterCols = 16384;                 // forward: longest row that is kept in registers
+constexpr int64_t kLnBackwardCols = 8192;                  // backward: longest row whose sums over the rows are
 
-// The sum over a CTA, the same in every thread, in an order that depends only on the launch's shape.
-__device__ __forceinline__ float cta_sum(float v, float *scratch)
+// How a thread's eight elements of a piece lie in the row.
+enum { kWide = 0, kStrided = 1, kChunk = 2 };              // 16-byte accesses; 32 apart; neighbours, element by element
+
+// First element of piece i for a thread; the others follow at distance 1 (kWide, kChunk) or 32 (kStrided).
+template <int TPR, int MAP> __device__ __forceinline__ int64_t piece_at(int i, int t)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if constexpr (MAP == kStrided) return (int64_t)(i * (TPR / 32) + (t >> 5)) * 256 + (t & 31);
+    return (int64_t)(i * TPR + t) * 8;
+}
+template <int MAP> __device__ __forceinline__ int piece_step() { return MAP == kStrided ? 32 : 1; }
+
+// Bytes of a ring's slot: a row and the rest of its first and last granule.
+__host__ __device__ __forceinline__ int slot_bytes(int64_t cols, int bytes) { return (int)((cols * bytes + 15) / 16 * 16 + 16); }
+
+// Starts the copy of row `row` into a slot, by `threads` threads.  A granule that reaches out of the matrix is copied element by
+// element (the first of the first row, the last of the last row).
+template <int DT> __device__ __forceinline__ void fetch_row(unsigned char *slot, const void *base, int64_t row, int64_t rows, int64_t cols,
+                                                            int64_t ld, int thread, int threads)
+{
+    constexpr int E = Elem<DT>::BYTES;
+    const uintptr_t begin = (uintptr_t)base + row * ld * E, end = begin + cols * E, first = begin & ~(uintptr_t)15;
+    const uintptr_t matrix_end = (uintptr_t)base + ((rows - 1) * ld + cols) * E;
+    const int granules = (int)((end - first + 15) >> 4);
+    for (int g = thread; g < granules; g += threads) {
+        const uintptr_t at = first + 16 * (uintptr_t)g;
+        if (at >= (uintptr_t)base && at + 16 <= matrix_end) {
+            copy_async16(smem_address(slot + 16 * g), (const void *)at);
+        } else {
+            for (int k = 0; k < 16; k += E)
+                if (at + k >= (uintptr_t)base && at + k + E <= matrix_end) {
+                    if constexpr (DT == UQ_BF16) *(unsigned short *)(slot + 16 * g + k) = *(const unsigned short *)(at + k);
+                    else *(float *)(slot + 16 * g + k) = *(const float *)(at + k);
+                }
+        }
+    }
+}
+__device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void fetch_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(PENDING) : "memory"); }
+
+// Eight elements of a row in shared memory, 0 beyond its end.
+template <int DT, int MAP> __device__ __forceinline__ void load_piece(const unsigned char *row, int at, int cols, float (&v)[8])
+{
+    if (MAP == kWide && at + 8 <= cols) {
+        if constexpr (DT == UQ_BF16) {
+            Elem<UQ_BF16>::unpack(*(const uint4 *)(row + at * 2), v);
+        } else {
+            const float4 lo = *(const float4 *)(row + at * 4), hi = *(const float4 *)(row + at * 4 + 16);
+            v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+        const int i = at + t * piece_step<MAP>();
+        v[t] = 0.0f;
+        if (i < cols) {
+            if constexpr (DT == UQ_BF16) v[t] = __uint_as_float((uint32_t)*(const unsigned short *)(row + i * 2) << 16);
+            else v[t] = *(const float *)(row + i * 4);
+        }
+    }
+}
+
+template <int DT, int MAP> __device__ __forceinline__ void store_piece(void *row, int64_t at, int64_t cols, const float (&v)[8])
+{
+    if constexpr (MAP == kStrided) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+            if (at + 32 * t < cols) store1<DT>(row, at + 32 * t, v[t]);
+    } else {
+        store8<DT>(row, at, (int)max((int64_t)0, min((int64_t)8, cols - at)), MAP == kWide, v);
+    }
+}
+
+// Eight weights, cached: every row reads them.
+template <int MAP> __device__ __forceinline__ void load_weights(const float *w, int64_t at, int64_t cols, bool wide, float (&v)[8])
+{
+    if (MAP != kStrided && wide && at + 8 <= cols) {
+        const float4 lo = __ldg((const float4 *)(w + at)), hi = __ldg((const float4 *)(w + at + 4));
+        v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+        return;
+    }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = at + t * piece_step<MAP>() < cols ? __ldg(w + at + t * piece_step<MAP>()) : 0.0f;
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    __syncthreads();
-    if (lane == 0) scratch[warp] = v;
-    __syncthreads();
+    return v;
+}
+
+// The sum over a row's threads, the same in each, in an order that depends only on TPR.  scratch: TPR / 32 floats that no
+// other sum uses until the next barrier but one.
+template <int TPR> __device__ __forceinline__ float row_sum(float v, float *scratch)
+{
+    v = warp_sum(v);
+    if constexpr (TPR > 32) {
+        if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < TPR / 32; ++w) v += scratch[w];
+    }
+    return v;
+}
+
+// Eight neighbouring results (zeros beyond the row) to codes; the four threads of a block are neighbours in a warp.
+template <int DT> __device__ __forceinline__ bool quantize_piece(const uq_mx &q, int64_t row, int64_t at, float (&v)[8])
+{
+    if constexpr (DT == UQ_BF16) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = __uint_as_float(bf16_bits(v[t]) << 16);
+    }
+    uint32_t m = max_abs_bits(v);
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+    const uint32_t byte = mx_scale_byte(m);
+    uint32_t codes = 0;
+    if (byte != 255u) {
+        const float inv = mx_inverse(byte);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] *= inv;
+        codes = e2m1x8_nearest(v);
+    }
+    const int64_t kt = mx_ktiles(q.cols);
+    if (at < mx_blocks(q.cols) * 32) *(uint32_t *)(q.codes + row * q.code_stride + (at >> 1)) = codes;
+    if ((at & 31) == 0 && at < kt * 128) q.scales[mx_scale_at(row, at >> 5, kt)] = (uint8_t)byte;
+    return byte == 255u;
+}
+
+struct NormArgs {
+    const void *x;
+    const float *gamma, *beta;
+    void *y;
+    float *mean, *rstd;
+    uint32_t *status;
+    int64_t rows, cols, ld, y_ld;
+    float eps;
+    uq_mx q;
+};
+
+// ---- forward ------------------------------------------------------------------------------------
+
+// TPR threads per row (the CTA, or one of its four warps), NC pieces of eight elements each.
+template <int TPR> struct RowThreads {
+    static constexpr int kThreads = TPR == 32 ? 128 : TPR, kRows = kThreads / TPR;
+    // CTAs per SM that the grid counts on
+    static constexpr int kResident = 512 / kThreads;
+};
+
+template <int DT, int TPR, int NC, int MAP>
+__global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kResident) layer_norm_kernel(const NormArgs p)
+{
+    constexpr int R = RowThreads<TPR>::kRows;
+    __shared__ float scratch[2][TPR / 32];
+    extern __shared__ __align__(16) unsigned char ring[];
+    grid_dependency_prologue();
+    const int t = threadIdx.x % TPR, cols = (int)p.cols;
+    const int slot = slot_bytes(p.cols, Elem<DT>::BYTES);
+    unsigned char *mine = ring + threadIdx.x / TPR * kRing * slot;
+    const int64_t first = (int64_t)blockIdx.x * R + threadIdx.x / TPR, step = (int64_t)gridDim.x * R;
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) {
+        if (first + i * step < p.rows) fetch_row<DT>(mine + i * slot, p.x, first + i * step, p.rows, p.cols, p.ld, t, TPR);
+        fetch_commit();
+    }
+    float gamma[NC][8], beta[NC][8];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+        const int64_t at = piece_at<TPR, MAP>(i, t);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { gamma[i][k] = 1.0f; beta[i][k] = 0.0f; }
+        if (p.gamma != nullptr) load_weights<MAP>(p.gamma, at, p.cols, ((uintptr_t)p.gamma & 15) == 0, gamma[i]);
+        if (p.beta != nullptr) load_weights<MAP>(p.beta, at, p.cols, ((uintptr_t)p.beta & 15) == 0, beta[i]);
+    }
+    const float n = (float)p.cols;
+    bool bad = false;
+    fetch_wait<kRing - 1>();
+    if constexpr (TPR > 32) __syncthreads(); else __syncwarp();
+    int s = 0;
+    for (int64_t row = first; row < p.rows; row += step) {
+        const unsigned char *xr = mine + s * slot + (((uintptr_t)p.x + row * p.ld * Elem<DT>::BYTES) & 15);
+        float v[NC][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            load_piece<DT, MAP>(xr, (int)piece_at<TPR, MAP>(i, t), cols, v[i]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += v[i][k];
+        }
+        fetch_wait<kRing - 2>();                           // the next row; the sum's barrier shows it to all, and frees this row's slot
+        if constexpr (TPR == 32) __syncwarp();
+        const float mean = row_sum<TPR>(sum, scratch[0]) / n;
+        if (row + kRing * step < p.rows) fetch_row<DT>(mine + s * slot, p.x, row + kRing * step, p.rows, p.cols, p.ld, t, TPR);
+        fetch_commit();
+        s = s + 1 == kRing ? 0 : s + 1;
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int at = (int)piece_at<TPR, MAP>(i, t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[i][k] = at + k * piece_step<MAP>() < cols ? v[i][k] - mean : 0.0f;
+                sum = __fmaf_rn(v[i][k], v[i][k], sum);
+            }
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<TPR>(sum, scratch[1]) / n + p.eps);
+        if (t == 0) {
+            if (p.mean != nullptr) p.mean[row] = mean;
+            if (p.rstd != nullptr) p.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            const int64_t at = piece_at<TPR, MAP>(i, t);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * rstd * gamma[i][k] + beta[i][k];
+            if (p.y != nullptr) store_piece<DT, MAP>((char *)p.y + row * p.y_ld * Elem<DT>::BYTES, at, p.cols, v[i]);
+            if constexpr (MAP != kStrided) {
+                if (p.q.codes != nullptr) {
+                    const int64_t have = p.cols - at;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[i][k] = k < have ? v[i][k] : 0.0f;
+                    bad = quantize_piece<DT>(p.q, row, at, v[i]) || bad;
+                }
+            }
+        }
+    }
+    if (bad && p.status != nullptr) atomicOr(p.status, UQ_STATUS_NONFINITE);
+}
+
+// Rows of any length: read three times (the second and third time from the caches).
+template <int DT>
+__global__ void __launch_bounds__(kLnThreads) layer_norm_long_kernel(const NormArgs p)
+{
+    __shared__ float scratch[2][kLnThreads / 32];
+    grid_dependency_prologue();
+    const int64_t cols = p.cols, chunks = (cols + 7) >> 3;
+    const int64_t all = (mx_ktiles(cols) * 16 + 31) / 32 * 32;         // whole warps, and a row's last scale tile
+    const bool wide = ((uintptr_t)p.x & 15) == 0 && (p.ld * Elem<DT>::BYTES & 15) == 0;
+    const bool wide_y = ((uintptr_t)p.y & 15) == 0 && (p.y_ld * Elem<DT>::BYTES & 15) == 0;
+    const bool wide_g = ((uintptr_t)p.gamma & 15) == 0, wide_b = ((uintptr_t)p.beta & 15) == 0;
+    const float n = (float)cols;
+    const int64_t row = blockIdx.x;
+    const char *xr = (const char *)p.x + row * p.ld * Elem<DT>::BYTES;
     float s = 0.0f;
+    for (int64_t c = threadIdx.x; c < chunks; c += kLnThreads) {
+        float v[8];
+        load8<DT>(xr, c * 8, (int)min((int64_t)8, cols - c * 8), wide, v);
 #pragma unroll
-    for (int w = 0; w < kLnThreads / 32; ++w) s += scratch[w];
-    return s;
-}
-
-template <int DT>
-__global__ void __launch_bounds__(kLnThreads) layer_norm_kernel(const void *__restrict__ x, int64_t rows, int64_t cols, int64_t ld,
-                                                                const float *__restrict__ gamma, const float *__restrict__ beta, float eps,
-                                                                void *__restrict__ y, int64_t y_ld, float *mean_out, float *rstd_out,
-                                                                uq_mx q, uint32_t *status)
-{
-    __shared__ float scratch[kLnThreads / 32];
-    grid_dependency_prologue();
-    const bool wide = ((uintptr_t)x & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0;
-    const bool wide_y = ((uintptr_t)y & 15) == 0 && (y_ld * Elem<DT>::BYTES & 15) == 0;
-    const int64_t chunks = (cols + 7) >> 3;
-    const int64_t all = q.codes != nullptr ? mx_ktiles(cols) * 16 : (chunks + 31) / 32 * 32;
-    const float n = (float)cols;
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        float s = 0.0f;
-        for (int64_t c = threadIdx.x; c < chunks; c += kLnThreads) {
-            float v[8];
-            load8<DT>(x, row * ld + c * 8, (int)min((int64_t)8, cols - c * 8), wide, v);
+        for (int k = 0; k < 8; ++k) s += v[k];
+    }
+    const float mean = row_sum<kLnThreads>(s, scratch[0]) / n;
+    s = 0.0f;
+    for (int64_t c = threadIdx.x; c < chunks; c += kLnThreads) {
+        float v[8];
+        const int have = (int)min((int64_t)8, cols - c * 8);
+        load8<DT>(xr, c * 8, have, wide, v);
 #pragma unroll
-            for (int t = 0; t < 8; ++t) s += v[t];
-        }
-        const float mean = cta_sum(s, scratch) / n;
-        s = 0.0f;
-        for (int64_t c = threadIdx.x; c < chunks; c += kLnThreads) {
-            float v[8];
-            const int have = (int)min((int64_t)8, cols - c * 8);
-            load8<DT>(x, row * ld + c * 8, have, wide, v);
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                const float d = t < have ? v[t] - mean : 0.0f;
-                s = __fmaf_rn(d, d, s);
-            }
-        }
-        const float rstd = 1.0f / sqrtf(cta_sum(s, scratch) / n + eps);
-        if (threadIdx.x == 0) {
-            if (mean_out != nullptr) mean_out[row] = mean;
-            if (rstd_out != nullptr) rstd_out[row] = rstd;
-        }
-        for (int64_t c0 = threadIdx.x & ~31; c0 < all; c0 += kLnThreads) {
-            const int64_t c = c0 + (threadIdx.x & 31);
-            const int have = (int)max((int64_t)0, min((int64_t)8, cols - c * 8));
-            float v[8];
-            load8<DT>(x, row * ld + c * 8, have, wide, v);
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                if (t < have) {
-                    v[t] = (v[t] - mean) * rstd;
-                    if (gamma != nullptr) v[t] *= __ldg(gamma + c * 8 + t);
-                    if (beta != nullptr) v[t] += __ldg(beta + c * 8 + t);
-                }
-            }
-            if (y != nullptr) store8<DT>(y, row * y_ld + c * 8, have, wide_y, v);
-            if (q.codes != nullptr) {
-                if constexpr (DT == UQ_BF16) {
-#pragma unroll
-                    for (int t = 0; t < 8; ++t) v[t] = __uint_as_float(bf16_bits(v[t]) << 16);
-                }
-                uint32_t m = max_abs_bits(v);
-                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-                const uint32_t byte = mx_scale_byte(m);
-                uint32_t codes = 0;
-                if (byte != 255u) {
-                    const float inv = mx_inverse(byte);
-#pragma unroll
-                    for (int t = 0; t < 8; ++t) v[t] *= inv;
-                    codes = e2m1x8_nearest(v);
-                } else if (status != nullptr) {
-                    atomicOr(status, UQ_STATUS_NONFINITE);
-                }
-                if (c < mx_blocks(cols) * 4) *(uint32_t *)(q.codes + row * q.code_stride + c * 4) = codes;
-                if ((c & 3) == 0 && c < all) q.scales[mx_scale_at(row, c >> 2, mx_ktiles(cols))] = (uint8_t)byte;
-            }
+        for (int k = 0; k < 8; ++k) {
+            const float d = k < have ? v[k] - mean : 0.0f;
+            s = __fmaf_rn(d, d, s);
         }
     }
+    const float rstd = 1.0f / sqrtf(row_sum<kLnThreads>(s, scratch[1]) / n + p.eps);
+    if (threadIdx.x == 0) {
+        if (p.mean != nullptr) p.mean[row] = mean;
+        if (p.rstd != nullptr) p.rstd[row] = rstd;
+    }
+    bool bad = false;
+    for (int64_t c = threadIdx.x; c < all; c += kLnThreads) {
+        const int have = (int)max((int64_t)0, min((int64_t)8, cols - c * 8));
+        float v[8], w[8];
+        load8<DT>(xr, c * 8, have, wide, v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = (v[k] - mean) * rstd;
+        if (p.gamma != nullptr) {
+            load_weights<kWide>(p.gamma, c * 8, cols, wide_g, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= w[k];
+        }
+        if (p.beta != nullptr) {
+            load_weights<kWide>(p.beta, c * 8, cols, wide_b, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] += w[k];
+        }
+        if (p.y != nullptr) store8<DT>((char *)p.y + row * p.y_ld * Elem<DT>::BYTES, c * 8, have, wide_y, v);
+        if (p.q.codes != nullptr) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = k < have ? v[k] : 0.0f;
+            bad = quantize_piece<DT>(p.q, row, c * 8, v) || bad;
+        }
+    }
+    if (bad && p.status != nullptr) atomicOr(p.status, UQ_STATUS_NONFINITE);
 }
 
-// A CTA takes every gridDim.x-th row; its sums for dgamma and dbeta are a row pair of `partial`, a thread's columns its own.
-template <int DT>
-__global__ void __launch_bounds__(kLnThreads) layer_norm_backward_kernel(const void *__restrict__ dy, int64_t dy_ld,
-                                                                         const void *__restrict__ x, int64_t x_ld, int64_t rows, int64_t cols,
-                                                                         const float *__restrict__ gamma, const float *__restrict__ mean_in,
-                                                                         const float *__restrict__ rstd_in, void *__restrict__ dx,
-                                                                         int64_t dx_ld, float *__restrict__ partial)
+// ---- backward -----------------------------------------------------------------------------------
+
+struct NormBackwardArgs {
+    const void *dy, *x;
+    const float *gamma, *mean, *rstd;
+    void *dx;
+    float *partial;                                        // [part][2][cols]: sums of dy xh and of dy over a part's rows
+    int64_t rows, cols, dy_ld, x_ld, dx_ld;
+};
+
+// A CTA takes every gridDim.x-th row (TPR = 32: its four warps one each) and keeps its sums over the rows in registers, a
+// thread's columns being its own.
+template <int DT, int TPR, int NC, int MAP>
+__global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kResident) layer_norm_backward_kernel(const NormBackwardArgs p)
 {
-    __shared__ float scratch[kLnThreads / 32];
+    constexpr int R = RowThreads<TPR>::kRows, T = RowThreads<TPR>::kThreads;
+    __shared__ float scratch[2][2][TPR / 32];
+    extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_prologue();
-    const bool wide_dy = ((uintptr_t)dy & 15) == 0 && (dy_ld * Elem<DT>::BYTES & 15) == 0;
-    const bool wide_x = ((uintptr_t)x & 15) == 0 && (x_ld * Elem<DT>::BYTES & 15) == 0;
-    const bool wide_dx = ((uintptr_t)dx & 15) == 0 && (dx_ld * Elem<DT>::BYTES & 15) == 0;
-    const int64_t chunks = (cols + 7) >> 3;
-    const float n = (float)cols;
-    float *pg = partial + (int64_t)blockIdx.x * 2 * cols, *pb = pg + cols;
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const float mean = __ldg(mean_in + row), rstd = __ldg(rstd_in + row);
+    const int t = threadIdx.x % TPR, part = threadIdx.x / TPR, cols = (int)p.cols;
+    const int slot = slot_bytes(p.cols, Elem<DT>::BYTES);
+    unsigned char *mine = ring + part * kRing * 2 * slot;
+    const int64_t first = (int64_t)blockIdx.x * R + part, step = (int64_t)gridDim.x * R;
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) {
+        if (first + i * step < p.rows) {
+            fetch_row<DT>(mine + 2 * i * slot, p.x, first + i * step, p.rows, p.cols, p.x_ld, t, TPR);
+            fetch_row<DT>(mine + (2 * i + 1) * slot, p.dy, first + i * step, p.rows, p.cols, p.dy_ld, t, TPR);
+        }
+        fetch_commit();
+    }
+    const float n = (float)p.cols;
+    const bool wide_g = ((uintptr_t)p.gamma & 15) == 0;
+    float dg[NC][8], db[NC][8];
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) dg[i][k] = db[i][k] = 0.0f;
+    fetch_wait<kRing - 1>();
+    if constexpr (TPR > 32) __syncthreads(); else __syncwarp();
+    int s = 0, turn = 0;
+    for (int64_t row = first; row < p.rows; row += step, turn ^= 1) {
+        const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
+        const unsigned char *xr = mine + 2 * s * slot + (((uintptr_t)p.x + row * p.x_ld * Elem<DT>::BYTES) & 15);
+        const unsigned char *dr = mine + (2 * s + 1) * slot + (((uintptr_t)p.dy + row * p.dy_ld * Elem<DT>::BYTES) & 15);
+        float d[NC][8], xh[NC][8];
         float s1 = 0.0f, s2 = 0.0f;
-        for (int64_t c = threadIdx.x; c < chunks; c += kLnThreads) {
-            const int have = (int)min((int64_t)8, cols - c * 8);
-            float d[8], v[8];
-            load8<DT>(dy, row * dy_ld + c * 8, have, wide_dy, d);
-            load8<DT>(x, row * x_ld + c * 8, have, wide_x, v);
 #pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                if (t < have) {
-                    const float xh = (v[t] - mean) * rstd, g = gamma != nullptr ? d[t] * __ldg(gamma + c * 8 + t) : d[t];
-                    s1 += g;
-                    s2 = __fmaf_rn(g, xh, s2);
-                }
+        for (int i = 0; i < NC; ++i) {                     // beyond the row dy is 0: nothing is added
+            const int at = (int)piece_at<TPR, MAP>(i, t);
+            load_piece<DT, MAP>(xr, at, cols, xh[i]);
+            load_piece<DT, MAP>(dr, at, cols, d[i]);
+            float w[8];
+            if (p.gamma != nullptr) load_weights<MAP>(p.gamma, at, p.cols, wide_g, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                xh[i][k] = at + k * piece_step<MAP>() < cols ? (xh[i][k] - mean) * rstd : 0.0f;
+                dg[i][k] = __fmaf_rn(d[i][k], xh[i][k], dg[i][k]);
+                db[i][k] += d[i][k];
+                if (p.gamma != nullptr) d[i][k] *= w[k];
+                s1 += d[i][k];
+                s2 = __fmaf_rn(d[i][k], xh[i][k], s2);
             }
         }
-        const float m1 = cta_sum(s1, scratch) / n, m2 = cta_sum(s2, scratch) / n;
-        const bool first = row == blockIdx.x;
-        for (int64_t c = threadIdx.x; c < chunks; c += kLnThreads) {
-            const int have = (int)min((int64_t)8, cols - c * 8);
-            float d[8], v[8];
-            load8<DT>(dy, row * dy_ld + c * 8, have, wide_dy, d);
-            load8<DT>(x, row * x_ld + c * 8, have, wide_x, v);
+        fetch_wait<kRing - 2>();                           // the next row; the barrier shows it to all, and frees this row's slot
+        s1 = warp_sum(s1);
+        s2 = warp_sum(s2);
+        if constexpr (TPR > 32) {
+            if ((threadIdx.x & 31) == 0) { scratch[turn][0][threadIdx.x >> 5] = s1; scratch[turn][1][threadIdx.x >> 5] = s2; }
+            __syncthreads();
+            s1 = s2 = 0.0f;
 #pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                if (t < have) {
-                    const int64_t i = c * 8 + t;
-                    const float xh = (v[t] - mean) * rstd, g = gamma != nullptr ? d[t] * __ldg(gamma + i) : d[t];
-                    pg[i] = first ? d[t] * xh : __fmaf_rn(d[t], xh, pg[i]);
-                    pb[i] = first ? d[t] : pb[i] + d[t];
-                    v[t] = rstd * (g - m1 - xh * m2);
-                }
-            }
-            if (dx != nullptr) store8<DT>(dx, row * dx_ld + c * 8, have, wide_dx, v);
+            for (int w = 0; w < TPR / 32; ++w) { s1 += scratch[turn][0][w]; s2 += scratch[turn][1][w]; }
+        } else {
+            __syncwarp();
         }
+        if (row + kRing * step < p.rows) {
+            fetch_row<DT>(mine + 2 * s * slot, p.x, row + kRing * step, p.rows, p.cols, p.x_ld, t, TPR);
+            fetch_row<DT>(mine + (2 * s + 1) * slot, p.dy, row + kRing * step, p.rows, p.cols, p.dy_ld, t, TPR);
+        }
+        fetch_commit();
+        s = s + 1 == kRing ? 0 : s + 1;
+        if (p.dx != nullptr) {
+            const float m1 = s1 / n, m2 = s2 / n;
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) d[i][k] = rstd * (d[i][k] - m1 - xh[i][k] * m2);
+                store_piece<DT, MAP>((char *)p.dx + row * p.dx_ld * Elem<DT>::BYTES, piece_at<TPR, MAP>(i, t), p.cols, d[i]);
+            }
+        }
+    }
+    float *out = p.partial + (int64_t)blockIdx.x * 2 * p.cols;
+    if constexpr (TPR == 32) {                             // the warps' sums, in their order
+        float *sums = (float *)ring;
+        __syncthreads();
+        for (int w = 0; w < R; ++w) {
+            if (part == w) {
+#pragma unroll
+                for (int i = 0; i < NC; ++i)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int c = (int)piece_at<TPR, MAP>(i, t) + k * piece_step<MAP>();
+                        if (c < cols) {
+                            sums[c] = w == 0 ? dg[i][k] : sums[c] + dg[i][k];
+                            sums[cols + c] = w == 0 ? db[i][k] : sums[cols + c] + db[i][k];
+                        }
+                    }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < 2 * cols; c += T) out[c] = sums[c];
+    } else {
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int c = (int)piece_at<TPR, MAP>(i, t) + k * piece_step<MAP>();
+                if (c < cols) { out[c] = dg[i][k]; out[cols + c] = db[i][k]; }
+            }
     }
 }
 
-// The partial sums of all CTAs, in their order.
-template <int GT>
-__global__ void __launch_bounds__(kLnThreads) weight_gradient_kernel(const float *__restrict__ partial, int parts, int64_t cols, void *dgamma,
-                                                                     void *dbeta)
+// Rows of any length: dx, each row read twice (the second time from the caches).
+template <int DT>
+__global__ void __launch_bounds__(kLnThreads) layer_norm_backward_long_kernel(const NormBackwardArgs p)
+{
+    __shared__ float scratch[2][kLnThreads / 32];
+    grid_dependency_prologue();
+    const int64_t cols = p.cols, chunks = (cols + 7) >> 3;
+    const bool wide_dy = ((uintptr_t)p.dy & 15) == 0 && (p.dy_ld * Elem<DT>::BYTES & 15) == 0;
+    const bool wide_x = ((uintptr_t)p.x & 15) == 0 && (p.x_ld * Elem<DT>::BYTES & 15) == 0;
+    const bool wide_dx = ((uintptr_t)p.dx & 15) == 0 && (p.dx_ld * Elem<DT>::BYTES & 15) == 0;
+    const bool wide_g = ((uintptr_t)p.gamma & 15) == 0;
+    const float n = (float)cols;
+    const int64_t row = blockIdx.x;
+    const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
+    const char *xr = (const char *)p.x + row * p.x_ld * Elem<DT>::BYTES, *dr = (const char *)p.dy + row * p.dy_ld * Elem<DT>::BYTES;
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int64_t c = threadIdx.x; c < chunks; c += kLnThreads) {
+        const int have = (int)min((int64_t)8, cols - c * 8);
+        float d[8], v[8], w[8];
+        load8<DT>(dr, c * 8, have, wide_dy, d);
+        load8<DT>(xr, c * 8, have, wide_x, v);
+        if (p.gamma != nullptr) load_weights<kWide>(p.gamma, c * 8, cols, wide_g, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k < have) {
+                const float g = p.gamma != nullptr ? d[k] * w[k] : d[k];
+                s1 += g;
+                s2 = __fmaf_rn(g, (v[k] - mean) * rstd, s2);
+            }
+        }
+    }
+    const float m1 = row_sum<kLnThreads>(s1, scratch[0]) / n, m2 = row_sum<kLnThreads>(s2, scratch[1]) / n;
+    for (int64_t c = threadIdx.x; c < chunks; c += kLnThreads) {
+        const int have = (int)min((int64_t)8, cols - c * 8);
+        float d[8], v[8], w[8];
+        load8<DT>(dr, c * 8, have, wide_dy, d);
+        load8<DT>(xr, c * 8, have, wide_x, v);
+        if (p.gamma != nullptr) load_weights<kWide>(p.gamma, c * 8, cols, wide_g, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float g = p.gamma != nullptr ? d[k] * w[k] : d[k];
+            v[k] = rstd * (g - m1 - (v[k] - mean) * rstd * m2);
+        }
+        store8<DT>((char *)p.dx + row * p.dx_ld * Elem<DT>::BYTES, c * 8, have, wide_dx, v);
+    }
+}
+
+// ... and the sums over the rows: a CTA takes 512 columns (two neighbours per thread, or two 256 apart) of every `parts`-th row.
+template <int DT, bool PAIRS>
+__global__ void __launch_bounds__(kLnThreads) weight_partials_kernel(const NormBackwardArgs p, int parts)
 {
     grid_dependency_prologue();
-    const int64_t c = (int64_t)blockIdx.x * kLnThreads + threadIdx.x;
-    if (c >= cols) return;
-    float g = 0.0f, b = 0.0f;
-    for (int p = 0; p < parts; ++p) {
-        g += partial[(int64_t)p * 2 * cols + c];
-        b += partial[(int64_t)p * 2 * cols + cols + c];
+    const int64_t strips = (p.cols + 511) / 512;
+    const int64_t part = blockIdx.x / strips, c = blockIdx.x % strips * 512 + (PAIRS ? 2 : 1) * threadIdx.x;
+    const int64_t c2 = PAIRS ? c + 1 : c + 256;
+    float g[2] = {0.0f, 0.0f}, b[2] = {0.0f, 0.0f};
+    if (c < p.cols) {
+#pragma unroll 4
+        for (int64_t row = part; row < p.rows; row += parts) {
+            const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
+            float x[2] = {0.0f, 0.0f}, d[2] = {0.0f, 0.0f};
+            if constexpr (DT == UQ_BF16) {
+                const unsigned short *xr = (const unsigned short *)p.x + row * p.x_ld, *dr = (const unsigned short *)p.dy + row * p.dy_ld;
+                if (PAIRS && c2 < p.cols) {
+                    const uint32_t xw = __ldg((const uint32_t *)(xr + c)), dw = __ldg((const uint32_t *)(dr + c));
+                    x[0] = bf16lo(xw); x[1] = bf16hi(xw); d[0] = bf16lo(dw); d[1] = bf16hi(dw);
+                } else {
+                    x[0] = __uint_as_float((uint32_t)__ldg(xr + c) << 16); d[0] = __uint_as_float((uint32_t)__ldg(dr + c) << 16);
+                    if (c2 < p.cols) { x[1] = __uint_as_float((uint32_t)__ldg(xr + c2) << 16); d[1] = __uint_as_float((uint32_t)__ldg(dr + c2) << 16); }
+                }
+            } else {
+                const float *xr = (const float *)p.x + row * p.x_ld, *dr = (const float *)p.dy + row * p.dy_ld;
+                x[0] = __ldg(xr + c); d[0] = __ldg(dr + c);
+                if (c2 < p.cols) { x[1] = __ldg(xr + c2); d[1] = __ldg(dr + c2); }
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                g[k] = __fmaf_rn(d[k], (x[k] - mean) * rstd, g[k]);
+                b[k] += d[k];
+            }
+        }
+        float *out = p.partial + part * 2 * p.cols;
+        out[c] = g[0]; out[p.cols + c] = b[0];
+        if (c2 < p.cols) { out[c2] = g[1]; out[p.cols + c2] = b[1]; }
     }
-    if (dgamma != nullptr) store1<GT>(dgamma, c, g);
-    if (dbeta != nullptr) store1<GT>(dbeta, c, b);
 }
 
-int backward_parts(int64_t rows) { return (int)min(rows, (int64_t)kLnGrid); }
+// The parts' sums: 32 columns per CTA; thread row y adds up every 16th part, then the 16 are added in order.
+template <int GT>
+__global__ void __launch_bounds__(512) weight_gradient_kernel(const float *__restrict__ partial, int parts, int64_t cols, void *dgamma,
+                                                              void *dbeta)
+{
+    __shared__ float s[16][33];
+    grid_dependency_prologue();
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int64_t c = (int64_t)(blockIdx.x >> 1) * 32 + x;
+    const bool beta = blockIdx.x & 1;
+    const float *src = partial + (beta ? cols : 0) + c;
+    float v = 0.0f;
+    if (c < cols) {
+#pragma unroll 8
+        for (int i = y; i < parts; i += 16) v += src[(int64_t)i * 2 * cols];
+    }
+    s[y][x] = v;
+    __syncthreads();
+    if (y == 0 && c < cols) {
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v += s[i][x];
+        void *out = beta ? dbeta : dgamma;
+        if (out != nullptr) store1<GT>(out, c, v);
+    }
+}
+
+// Threads per row of the backward pass.
+int backward_threads(int64_t cols) { return cols <= 512 ? 32 : cols <= 1024 ? 64 : cols <= 2048 ? 128 : cols <= 4096 ? 256 : 512; }
+
+// CTAs of the backward pass, each of which leaves a part: enough to fill the GPU, and four rows for each CTA or each of its warps.
+int backward_parts(int64_t rows, int64_t cols)
+{
+    if (cols > kLnBackwardCols) return (int)min((rows + 63) / 64, (int64_t)64);
+    const int threads = backward_threads(cols), fewest = threads == 32 ? 16 : 4;
+    return (int)min((rows + fewest - 1) / fewest, (int64_t)148 * (512 / (threads == 32 ? 128 : threads)));
+}
+
+template <int DT> bool rows_wide(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0; }
+
+template <typename K, typename A> void launch_rows(K *kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, const A &args)
+{
+    if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    launch_k_smem(kernel, dim3((unsigned)grid), dim3(threads), smem, st, args);
+}
+
+template <int DT, int TPR, int NC> void launch_forward(const NormArgs &p, int map, cudaStream_t st)
+{
+    using T = RowThreads<TPR>;
+    const int64_t grid = min((p.rows + T::kRows - 1) / T::kRows, (int64_t)148 * T::kResident);
+    const size_t smem = (size_t)T::kRows * kRing * slot_bytes(p.cols, Elem<DT>::BYTES);
+    if (map == kWide) launch_rows(layer_norm_kernel<DT, TPR, NC, kWide>, grid, T::kThreads, smem, st, p);
+    else if (map == kStrided) launch_rows(layer_norm_kernel<DT, TPR, NC, kStrided>, grid, T::kThreads, smem, st, p);
+    else launch_rows(layer_norm_kernel<DT, TPR, NC, kChunk>, grid, T::kThreads, smem, st, p);
+}
+
+template <int DT> void launch_forward_any(const NormArgs &p, cudaStream_t st)
+{
+    const bool wide = rows_wide<DT>(p.x, p.ld) && (p.y == nullptr || rows_wide<DT>(p.y, p.y_ld));
+    const int map = wide ? kWide : p.q.codes == nullptr ? kStrided : kChunk;
+    if (p.cols <= 256) launch_forward<DT, 32, 1>(p, map, st);
+    else if (p.cols <= 512) launch_forward<DT, 32, 2>(p, map, st);
+    else if (p.cols <= 1024) launch_forward<DT, 64, 2>(p, map, st);
+    else if (p.cols <= 2048) launch_forward<DT, 128, 2>(p, map, st);
+    else if (p.cols <= 4096) launch_forward<DT, 128, 4>(p, map, st);
+    else if (p.cols <= 8192) launch_forward<DT, 256, 4>(p, map, st);
+    else if (p.cols <= kLnRegisterCols) launch_forward<DT, 512, 4>(p, map, st);
+    else launch_k(layer_norm_long_kernel<DT>, dim3((unsigned)p.rows), dim3(kLnThreads), st, p);
+}
+
+template <int DT, int TPR, int NC> void launch_backward(const NormBackwardArgs &p, bool wide, int parts, cudaStream_t st)
+{
+    using T = RowThreads<TPR>;
+    const size_t smem = (size_t)T::kRows * kRing * 2 * slot_bytes(p.cols, Elem<DT>::BYTES);
+    if (wide) launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kWide>, parts, T::kThreads, smem, st, p);
+    else launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kStrided>, parts, T::kThreads, smem, st, p);
+}
+
+template <int DT> void launch_backward_any(const NormBackwardArgs &p, int parts, bool sums, cudaStream_t st)
+{
+    const bool wide = rows_wide<DT>(p.dy, p.dy_ld) && rows_wide<DT>(p.x, p.x_ld) && (p.dx == nullptr || rows_wide<DT>(p.dx, p.dx_ld));
+    if (p.cols <= 256) launch_backward<DT, 32, 1>(p, wide, parts, st);
+    else if (p.cols <= 512) launch_backward<DT, 32, 2>(p, wide, parts, st);
+    else if (p.cols <= 1024) launch_backward<DT, 64, 2>(p, wide, parts, st);
+    else if (p.cols <= 2048) launch_backward<DT, 128, 2>(p, wide, parts, st);
+    else if (p.cols <= 4096) launch_backward<DT, 256, 2>(p, wide, parts, st);
+    else if (p.cols <= kLnBackwardCols) launch_backward<DT, 512, 2>(p, wide, parts, st);
+    else {
+        if (p.dx != nullptr) launch_k(layer_norm_backward_long_kernel<DT>, dim3((unsigned)p.rows), dim3(kLnThreads), st, p);
+        if (sums) {
+            const dim3 grid((unsigned)((p.cols + 511) / 512 * parts));
+            if (DT == UQ_BF16 && wide) launch_k(weight_partials_kernel<DT, true>, grid, dim3(kLnThreads), st, p, parts);
+            else launch_k(weight_partials_kernel<DT, false>, grid, dim3(kLnThreads), st, p, parts);
+        }
+    }
+}
 
 }  // namespace
 
-size_t layer_norm_workspace_bytes(int64_t rows, int64_t cols) { return (size_t)backward_parts(rows) * 2 * cols * sizeof(float); }
+size_t layer_norm_workspace_bytes(int64_t rows, int64_t cols) { return (size_t)backward_parts(rows, cols) * 2 * cols * sizeof(float); }
 
 cudaError_t launch_layer_norm(const void *x, int64_t rows, int64_t cols, int64_t ld, int dtype, const float *gamma, const float *beta,
                               float eps, void *y, int64_t y_ld, float *mean, float *rstd, const uq_mx &q, uint32_t *status,
                               cudaStream_t st)
 {
-    const dim3 grid((unsigned)min(rows, (int64_t)148 * 8));
-    if (dtype == UQ_BF16)
-        launch_k(layer_norm_kernel<UQ_BF16>, grid, dim3(kLnThreads), st, x, rows, cols, ld, gamma, beta, eps, y, y_ld, mean, rstd, q, status);
-    else
-        launch_k(layer_norm_kernel<UQ_F32>, grid, dim3(kLnThreads), st, x, rows, cols, ld, gamma, beta, eps, y, y_ld, mean, rstd, q, status);
+    const NormArgs p = {x, gamma, beta, y, mean, rstd, status, rows, cols, ld, y_ld, eps, q};
+    if (dtype == UQ_BF16) launch_forward_any<UQ_BF16>(p, st);
+    else launch_forward_any<UQ_F32>(p, st);
     return cudaGetLastError();
 }
 
@@ -200,21 +643,19 @@ cudaError_t launch_layer_norm_backward(const void *dy, int64_t dy_ld, const void
                                        const float *gamma, const float *mean, const float *rstd, void *dx, int64_t dx_ld, void *dgamma,
                                        void *dbeta, int grad_dtype, void *workspace, cudaStream_t st)
 {
-    const int parts = backward_parts(rows);
+    const int parts = backward_parts(rows, cols);
     float *partial = (float *)workspace;
     if (rows > 0) {
-        if (dtype == UQ_BF16)
-            launch_k(layer_norm_backward_kernel<UQ_BF16>, dim3(parts), dim3(kLnThreads), st, dy, dy_ld, x, x_ld, rows, cols, gamma, mean, rstd,
-                     dx, dx_ld, partial);
-        else
-            launch_k(layer_norm_backward_kernel<UQ_F32>, dim3(parts), dim3(kLnThreads), st, dy, dy_ld, x, x_ld, rows, cols, gamma, mean, rstd,
-                     dx, dx_ld, partial);
+        const NormBackwardArgs p = {dy, x, gamma, mean, rstd, dx, partial, rows, cols, dy_ld, x_ld, dx_ld};
+        const bool sums = dgamma != nullptr || dbeta != nullptr;
+        if (dtype == UQ_BF16) launch_backward_any<UQ_BF16>(p, parts, sums, st);
+        else launch_backward_any<UQ_F32>(p, parts, sums, st);
         if (cudaError_t e = cudaGetLastError()) return e;
     }
     if (dgamma == nullptr && dbeta == nullptr) return cudaSuccess;
-    const dim3 grid((unsigned)((cols + kLnThreads - 1) / kLnThreads));
-    if (grad_dtype == UQ_BF16) launch_k(weight_gradient_kernel<UQ_BF16>, grid, dim3(kLnThreads), st, (const float *)partial, parts, cols, dgamma, dbeta);
-    else launch_k(weight_gradient_kernel<UQ_F32>, grid, dim3(kLnThreads), st, (const float *)partial, parts, cols, dgamma, dbeta);
+    const dim3 grid((unsigned)((cols + 31) / 32 * 2));
+    if (grad_dtype == UQ_BF16) launch_k(weight_gradient_kernel<UQ_BF16>, grid, dim3(512), st, (const float *)partial, parts, cols, dgamma, dbeta);
+    else launch_k(weight_gradient_kernel<UQ_F32>, grid, dim3(512), st, (const float *)partial, parts, cols, dgamma, dbeta);
     return cudaGetLastError();
 }
 

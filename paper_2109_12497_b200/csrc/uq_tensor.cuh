@@ -8,8 +8,6 @@
 
 namespace uq {
 
-__device__ __forceinline__ uint32_t smem_address(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
 // ---- barriers -----------------------------------------------------------------------------------
 
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)

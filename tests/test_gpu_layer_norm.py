@@ -29,13 +29,13 @@ def cuda(v):
 
 
 def forward_bounds(x, gamma, beta, mean, rstd, cols):
-    """How far binary32 may be off, in units of u = 2^-24.  Sums are trees or chains of at most L = cols / 256 + 16 additions
-    per partial value (8 values a thread and step, 256 threads, then 13 levels):
+    """How far binary32 may be off, in units of u = 2^-24.  A value goes through at most L = cols / 256 + 53 additions: a chain
+    in its thread (32 values, or cols / 256 where rows are longer than a CTA holds), 5 levels in the warp, 16 warps:
       mean:  L u mean|x|, and u |mean| for the division
       var:   each square's factor is off by u |x - mean| + |error of the mean|; the sum and the division L + 4 more
       rstd:  half the relative error of var, and 2 u for root and division
       y:     |x - mean| rstd (rel. error of rstd + 4 u) + rstd |error of the mean|, times gamma, and u for each result."""
-    u, L = 2.0 ** -24, cols / 256 + 24
+    u, L = 2.0 ** -24, cols / 256 + 53
     e_mean = L * u * np.abs(x).mean(1) + u * np.abs(mean)
     c = np.abs(x - mean[:, None])
     var = (c ** 2).mean(1)
@@ -109,7 +109,7 @@ def backward_bounds(dy, x, gamma, mean, rstd, cols, rows):
       xh: 2 u relative to |x - mean| rstd, and u |x| rstd for the difference;  t: u relative
       the two means: (L + 4) u of the mean of magnitudes, with xh's error in the second
       dx: rstd (u-errors of its three terms);  dgamma: sum |dy| (error of xh + u |xh|) + R u sum |dy xh|;  dbeta: R u sum |dy|."""
-    u, L = 2.0 ** -24, cols / 256 + 24
+    u, L = 2.0 ** -24, cols / 256 + 53
     c = np.abs(x - mean[:, None])
     xh = c * rstd[:, None]
     e_xh = 3 * u * xh
