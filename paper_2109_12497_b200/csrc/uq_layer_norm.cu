@@ -45,6 +45,12 @@ template <int DT> __device__ __forceinline__ void fetch_row(unsigned char *slot,
     const uintptr_t begin = (uintptr_t)base + row * ld * E, end = begin + cols * E, first = begin & ~(uintptr_t)15;
     const uintptr_t matrix_end = (uintptr_t)base + ((rows - 1) * ld + cols) * E;
     const int granules = (int)((end - first + 15) >> 4);
+    if (first >= (uintptr_t)base && first + 16 * (uintptr_t)granules <= matrix_end) {
+        const uint32_t dst = smem_address(slot);
+#pragma unroll 4
+        for (int g = thread; g < granules; g += threads) copy_async16(dst + 16 * g, (const void *)(first + 16 * g));
+        return;
+    }
     for (int g = thread; g < granules; g += threads) {
         const uintptr_t at = first + 16 * (uintptr_t)g;
         if (at >= (uintptr_t)base && at + 16 <= matrix_end) {
@@ -107,6 +113,49 @@ template <int MAP> __device__ __forceinline__ void load_weights(const float *w, 
     for (int t = 0; t < 8; ++t) v[t] = at + t * piece_step<MAP>() < cols ? __ldg(w + at + t * piece_step<MAP>()) : 0.0f;
 }
 
+// Two values per instruction: the row's elements are held in pairs.
+__device__ __forceinline__ uint64_t pair_bits(float2 v)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 pair_of(uint64_t r)
+{
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(r));
+    return v;
+}
+__device__ __forceinline__ float2 operator+(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 operator*(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(pair_bits(a)), "l"(pair_bits(b)), "l"(pair_bits(c)));
+    return pair_of(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ void to_pairs(const float (&v)[8], float2 (&w)[4])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = make_float2(v[2 * k], v[2 * k + 1]);
+}
+__device__ __forceinline__ void from_pairs(const float2 (&w)[4], float (&v)[8])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { v[2 * k] = w[k].x; v[2 * k + 1] = w[k].y; }
+}
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
@@ -122,11 +171,43 @@ template <int TPR> __device__ __forceinline__ float row_sum(float v, float *scra
     if constexpr (TPR > 32) {
         if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
         __syncthreads();
-        v = 0.0f;
+        if constexpr (TPR == 64) return scratch[0] + scratch[1];
+        float2 s = both(0.0f);
 #pragma unroll
-        for (int w = 0; w < TPR / 32; ++w) v += scratch[w];
+        for (int w = 0; w < TPR / 32; w += 4) {
+            const float4 q = *(const float4 *)(scratch + w);
+            s = (s + make_float2(q.x, q.y)) + make_float2(q.z, q.w);
+        }
+        v = s.x + s.y;
     }
     return v;
+}
+
+// Two sums at once.
+template <int TPR> __device__ __forceinline__ float2 row_sums(float2 v, float2 *scratch)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = v + make_float2(__shfl_xor_sync(0xFFFFFFFFu, v.x, o), __shfl_xor_sync(0xFFFFFFFFu, v.y, o));
+    if constexpr (TPR > 32) {
+        if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
+        __syncthreads();
+        v = both(0.0f);
+#pragma unroll
+        for (int w = 0; w < TPR / 32; w += 2) {
+            const float4 q = *(const float4 *)(scratch + w);
+            v = (v + make_float2(q.x, q.y)) + make_float2(q.z, q.w);
+        }
+    }
+    return v;
+}
+
+// 1 / sqrt(v): the approximation (2 units in the last place) and a Newton step, without the chains of an exact root and an exact
+// division in every thread; 0 and infinity keep their limits.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const float r = rsqrtf(v);
+    const float better = __fmaf_rn(0.5f * r, __fmaf_rn(-v * r, r, 1.0f), r);
+    return r > 0.0f && r < __int_as_float(0x7F800000) ? better : r;
 }
 
 // Eight neighbouring results (zeros beyond the row) to codes; the four threads of a block are neighbours in a warp.
@@ -153,6 +234,18 @@ template <int DT> __device__ __forceinline__ bool quantize_piece(const uq_mx &q,
     return byte == 255u;
 }
 
+// Sets what lies beyond the row to 0.
+template <int MAP> __device__ __forceinline__ void clear_beyond(int at, int cols, float2 (&v)[4])
+{
+    if (at + 7 * piece_step<MAP>() >= cols) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (at + 2 * k * piece_step<MAP>() >= cols) v[k].x = 0.0f;
+            if (at + (2 * k + 1) * piece_step<MAP>() >= cols) v[k].y = 0.0f;
+        }
+    }
+}
+
 struct NormArgs {
     const void *x;
     const float *gamma, *beta;
@@ -177,7 +270,7 @@ template <int DT, int TPR, int NC, int MAP>
 __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kResident) layer_norm_kernel(const NormArgs p)
 {
     constexpr int R = RowThreads<TPR>::kRows;
-    __shared__ float scratch[2][TPR / 32];
+    __shared__ __align__(16) float scratch[2][TPR / 32];
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_prologue();
     const int t = threadIdx.x % TPR, cols = (int)p.cols;
@@ -189,47 +282,52 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         if (first + i * step < p.rows) fetch_row<DT>(mine + i * slot, p.x, first + i * step, p.rows, p.cols, p.ld, t, TPR);
         fetch_commit();
     }
-    float gamma[NC][8], beta[NC][8];
+    float2 gamma[NC][4], beta[NC][4];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
         const int64_t at = piece_at<TPR, MAP>(i, t);
+        float w[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { gamma[i][k] = 1.0f; beta[i][k] = 0.0f; }
-        if (p.gamma != nullptr) load_weights<MAP>(p.gamma, at, p.cols, ((uintptr_t)p.gamma & 15) == 0, gamma[i]);
-        if (p.beta != nullptr) load_weights<MAP>(p.beta, at, p.cols, ((uintptr_t)p.beta & 15) == 0, beta[i]);
+        for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+        if (p.gamma != nullptr) load_weights<MAP>(p.gamma, at, p.cols, ((uintptr_t)p.gamma & 15) == 0, w);
+        to_pairs(w, gamma[i]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = 0.0f;
+        if (p.beta != nullptr) load_weights<MAP>(p.beta, at, p.cols, ((uintptr_t)p.beta & 15) == 0, w);
+        to_pairs(w, beta[i]);
     }
-    const float n = (float)p.cols;
+    const float inv_n = 1.0f / (float)p.cols;
     bool bad = false;
     fetch_wait<kRing - 1>();
     if constexpr (TPR > 32) __syncthreads(); else __syncwarp();
     int s = 0;
     for (int64_t row = first; row < p.rows; row += step) {
         const unsigned char *xr = mine + s * slot + (((uintptr_t)p.x + row * p.ld * Elem<DT>::BYTES) & 15);
-        float v[NC][8];
-        float sum = 0.0f;
+        float2 v[NC][4], sum = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            load_piece<DT, MAP>(xr, (int)piece_at<TPR, MAP>(i, t), cols, v[i]);
+            float w[8];
+            load_piece<DT, MAP>(xr, (int)piece_at<TPR, MAP>(i, t), cols, w);
+            to_pairs(w, v[i]);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum += v[i][k];
+            for (int k = 0; k < 4; ++k) sum = sum + v[i][k];
         }
         fetch_wait<kRing - 2>();                           // the next row; the sum's barrier shows it to all, and frees this row's slot
         if constexpr (TPR == 32) __syncwarp();
-        const float mean = row_sum<TPR>(sum, scratch[0]) / n;
+        const float mean = row_sum<TPR>(sum.x + sum.y, scratch[0]) * inv_n;
         if (row + kRing * step < p.rows) fetch_row<DT>(mine + s * slot, p.x, row + kRing * step, p.rows, p.cols, p.ld, t, TPR);
         fetch_commit();
         s = s + 1 == kRing ? 0 : s + 1;
-        sum = 0.0f;
+        sum = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int at = (int)piece_at<TPR, MAP>(i, t);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[i][k] = at + k * piece_step<MAP>() < cols ? v[i][k] - mean : 0.0f;
-                sum = __fmaf_rn(v[i][k], v[i][k], sum);
-            }
+            for (int k = 0; k < 4; ++k) v[i][k] = v[i][k] + both(-mean);
+            clear_beyond<MAP>((int)piece_at<TPR, MAP>(i, t), cols, v[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum = fma2(v[i][k], v[i][k], sum);
         }
-        const float rstd = 1.0f / sqrtf(row_sum<TPR>(sum, scratch[1]) / n + p.eps);
+        const float rstd = inverse_root(row_sum<TPR>(sum.x + sum.y, scratch[1]) * inv_n + p.eps);
         if (t == 0) {
             if (p.mean != nullptr) p.mean[row] = mean;
             if (p.rstd != nullptr) p.rstd[row] = rstd;
@@ -238,15 +336,12 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         for (int i = 0; i < NC; ++i) {
             const int64_t at = piece_at<TPR, MAP>(i, t);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[i][k] = v[i][k] * rstd * gamma[i][k] + beta[i][k];
-            if (p.y != nullptr) store_piece<DT, MAP>((char *)p.y + row * p.y_ld * Elem<DT>::BYTES, at, p.cols, v[i]);
-            if constexpr (MAP != kStrided) {
-                if (p.q.codes != nullptr) {
-                    const int64_t have = p.cols - at;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[i][k] = k < have ? v[i][k] : 0.0f;
-                    bad = quantize_piece<DT>(p.q, row, at, v[i]) || bad;
-                }
+            for (int k = 0; k < 4; ++k) v[i][k] = fma2(v[i][k] * both(rstd), gamma[i][k], beta[i][k]);
+            float w[8];
+            from_pairs(v[i], w);
+            if (p.y != nullptr) store_piece<DT, MAP>((char *)p.y + row * p.y_ld * Elem<DT>::BYTES, at, p.cols, w);
+            if constexpr (MAP != kStrided) {             // (elements beyond the row are 0, and so is beta there)
+                if (p.q.codes != nullptr) bad = quantize_piece<DT>(p.q, row, at, w) || bad;
             }
         }
     }
@@ -257,7 +352,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
 template <int DT>
 __global__ void __launch_bounds__(kLnThreads) layer_norm_long_kernel(const NormArgs p)
 {
-    __shared__ float scratch[2][kLnThreads / 32];
+    __shared__ __align__(16) float scratch[2][kLnThreads / 32];
     grid_dependency_prologue();
     const int64_t cols = p.cols, chunks = (cols + 7) >> 3;
     const int64_t all = (mx_ktiles(cols) * 16 + 31) / 32 * 32;         // whole warps, and a row's last scale tile
@@ -334,7 +429,7 @@ template <int DT, int TPR, int NC, int MAP>
 __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kResident) layer_norm_backward_kernel(const NormBackwardArgs p)
 {
     constexpr int R = RowThreads<TPR>::kRows, T = RowThreads<TPR>::kThreads;
-    __shared__ float scratch[2][2][TPR / 32];
+    __shared__ __align__(16) float2 scratch[2][TPR / 32];
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_prologue();
     const int t = threadIdx.x % TPR, part = threadIdx.x / TPR, cols = (int)p.cols;
@@ -349,13 +444,13 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         }
         fetch_commit();
     }
-    const float n = (float)p.cols;
+    const float inv_n = 1.0f / (float)p.cols;
     const bool wide_g = ((uintptr_t)p.gamma & 15) == 0;
-    float dg[NC][8], db[NC][8];
+    float2 dg[NC][4], db[NC][4];
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dg[i][k] = db[i][k] = 0.0f;
+        for (int k = 0; k < 4; ++k) dg[i][k] = db[i][k] = both(0.0f);
     fetch_wait<kRing - 1>();
     if constexpr (TPR > 32) __syncthreads(); else __syncwarp();
     int s = 0, turn = 0;
@@ -363,37 +458,30 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
         const unsigned char *xr = mine + 2 * s * slot + (((uintptr_t)p.x + row * p.x_ld * Elem<DT>::BYTES) & 15);
         const unsigned char *dr = mine + (2 * s + 1) * slot + (((uintptr_t)p.dy + row * p.dy_ld * Elem<DT>::BYTES) & 15);
-        float d[NC][8], xh[NC][8];
-        float s1 = 0.0f, s2 = 0.0f;
+        float2 d[NC][4], xh[NC][4], sum1 = both(0.0f), sum2 = both(0.0f);
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {                     // beyond the row dy is 0: nothing is added
+        for (int i = 0; i < NC; ++i) {                     // beyond the row x and dy are 0: nothing is added
             const int at = (int)piece_at<TPR, MAP>(i, t);
-            load_piece<DT, MAP>(xr, at, cols, xh[i]);
-            load_piece<DT, MAP>(dr, at, cols, d[i]);
             float w[8];
-            if (p.gamma != nullptr) load_weights<MAP>(p.gamma, at, p.cols, wide_g, w);
+            float2 g[4];
+            load_piece<DT, MAP>(xr, at, cols, w);
+            to_pairs(w, xh[i]);
+            load_piece<DT, MAP>(dr, at, cols, w);
+            to_pairs(w, d[i]);
+            if (p.gamma != nullptr) { load_weights<MAP>(p.gamma, at, p.cols, wide_g, w); to_pairs(w, g); }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                xh[i][k] = at + k * piece_step<MAP>() < cols ? (xh[i][k] - mean) * rstd : 0.0f;
-                dg[i][k] = __fmaf_rn(d[i][k], xh[i][k], dg[i][k]);
-                db[i][k] += d[i][k];
-                if (p.gamma != nullptr) d[i][k] *= w[k];
-                s1 += d[i][k];
-                s2 = __fmaf_rn(d[i][k], xh[i][k], s2);
+            for (int k = 0; k < 4; ++k) {
+                xh[i][k] = (xh[i][k] + both(-mean)) * both(rstd);
+                dg[i][k] = fma2(d[i][k], xh[i][k], dg[i][k]);
+                db[i][k] = db[i][k] + d[i][k];
+                if (p.gamma != nullptr) d[i][k] = d[i][k] * g[k];
+                sum1 = sum1 + d[i][k];
+                sum2 = fma2(d[i][k], xh[i][k], sum2);
             }
         }
         fetch_wait<kRing - 2>();                           // the next row; the barrier shows it to all, and frees this row's slot
-        s1 = warp_sum(s1);
-        s2 = warp_sum(s2);
-        if constexpr (TPR > 32) {
-            if ((threadIdx.x & 31) == 0) { scratch[turn][0][threadIdx.x >> 5] = s1; scratch[turn][1][threadIdx.x >> 5] = s2; }
-            __syncthreads();
-            s1 = s2 = 0.0f;
-#pragma unroll
-            for (int w = 0; w < TPR / 32; ++w) { s1 += scratch[turn][0][w]; s2 += scratch[turn][1][w]; }
-        } else {
-            __syncwarp();
-        }
+        if constexpr (TPR == 32) __syncwarp();
+        const float2 m = row_sums<TPR>(make_float2(sum1.x + sum1.y, sum2.x + sum2.y), scratch[turn]) * both(inv_n);
         if (row + kRing * step < p.rows) {
             fetch_row<DT>(mine + 2 * s * slot, p.x, row + kRing * step, p.rows, p.cols, p.x_ld, t, TPR);
             fetch_row<DT>(mine + (2 * s + 1) * slot, p.dy, row + kRing * step, p.rows, p.cols, p.dy_ld, t, TPR);
@@ -401,12 +489,13 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         fetch_commit();
         s = s + 1 == kRing ? 0 : s + 1;
         if (p.dx != nullptr) {
-            const float m1 = s1 / n, m2 = s2 / n;
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
+                float w[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) d[i][k] = rstd * (d[i][k] - m1 - xh[i][k] * m2);
-                store_piece<DT, MAP>((char *)p.dx + row * p.dx_ld * Elem<DT>::BYTES, piece_at<TPR, MAP>(i, t), p.cols, d[i]);
+                for (int k = 0; k < 4; ++k) d[i][k] = both(rstd) * fma2(xh[i][k], both(-m.y), d[i][k] + both(-m.x));
+                from_pairs(d[i], w);
+                store_piece<DT, MAP>((char *)p.dx + row * p.dx_ld * Elem<DT>::BYTES, piece_at<TPR, MAP>(i, t), p.cols, w);
             }
         }
     }
@@ -417,27 +506,35 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         for (int w = 0; w < R; ++w) {
             if (part == w) {
 #pragma unroll
-                for (int i = 0; i < NC; ++i)
+                for (int i = 0; i < NC; ++i) {
+                    float g[8], b[8];
+                    from_pairs(dg[i], g);
+                    from_pairs(db[i], b);
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const int c = (int)piece_at<TPR, MAP>(i, t) + k * piece_step<MAP>();
                         if (c < cols) {
-                            sums[c] = w == 0 ? dg[i][k] : sums[c] + dg[i][k];
-                            sums[cols + c] = w == 0 ? db[i][k] : sums[cols + c] + db[i][k];
+                            sums[c] = w == 0 ? g[k] : sums[c] + g[k];
+                            sums[cols + c] = w == 0 ? b[k] : sums[cols + c] + b[k];
                         }
                     }
+                }
             }
             __syncthreads();
         }
         for (int c = threadIdx.x; c < 2 * cols; c += T) out[c] = sums[c];
     } else {
 #pragma unroll
-        for (int i = 0; i < NC; ++i)
+        for (int i = 0; i < NC; ++i) {
+            float g[8], b[8];
+            from_pairs(dg[i], g);
+            from_pairs(db[i], b);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int c = (int)piece_at<TPR, MAP>(i, t) + k * piece_step<MAP>();
-                if (c < cols) { out[c] = dg[i][k]; out[cols + c] = db[i][k]; }
+                if (c < cols) { out[c] = g[k]; out[cols + c] = b[k]; }
             }
+        }
     }
 }
 
@@ -445,7 +542,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
 template <int DT>
 __global__ void __launch_bounds__(kLnThreads) layer_norm_backward_long_kernel(const NormBackwardArgs p)
 {
-    __shared__ float scratch[2][kLnThreads / 32];
+    __shared__ __align__(16) float scratch[2][kLnThreads / 32];
     grid_dependency_prologue();
     const int64_t cols = p.cols, chunks = (cols + 7) >> 3;
     const bool wide_dy = ((uintptr_t)p.dy & 15) == 0 && (p.dy_ld * Elem<DT>::BYTES & 15) == 0;

@@ -31,12 +31,13 @@ def cuda(v):
 def forward_bounds(x, gamma, beta, mean, rstd, cols):
     """How far binary32 may be off, in units of u = 2^-24.  A value goes through at most L = cols / 256 + 53 additions: a chain
     in its thread (32 values, or cols / 256 where rows are longer than a CTA holds), 5 levels in the warp, 16 warps:
-      mean:  L u mean|x|, and u |mean| for the division
-      var:   each square's factor is off by u |x - mean| + |error of the mean|; the sum and the division L + 4 more
-      rstd:  half the relative error of var, and 2 u for root and division
+      mean:  L u mean|x|, and 2 u |mean| for 1 / cols and the product with it
+      var:   each square's factor is off by u |x - mean| + |error of the mean|; the sum and the product L + 4 more
+      rstd:  half the relative error of var, u for adding eps, 3 u for the root (an approximation of 2 units in the last place,
+             4 u, whose square, 24 u^2, is left by a Newton step of three roundings)
       y:     |x - mean| rstd (rel. error of rstd + 4 u) + rstd |error of the mean|, times gamma, and u for each result."""
     u, L = 2.0 ** -24, cols / 256 + 53
-    e_mean = L * u * np.abs(x).mean(1) + u * np.abs(mean)
+    e_mean = L * u * np.abs(x).mean(1) + 2 * u * np.abs(mean)
     c = np.abs(x - mean[:, None])
     var = (c ** 2).mean(1)
     e_var = 2 * (c * (u * c + e_mean[:, None])).mean(1) + e_mean ** 2 + (L + 4) * u * var
