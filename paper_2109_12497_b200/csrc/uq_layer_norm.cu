@@ -22,10 +22,12 @@ constexpr int kRing = 3;                                   // rows in shared mem
 constexpr int64_t kLnRegisterCols = 16384;                 // forward: longest row that is kept in registers
 constexpr int64_t kLnBackwardCols = 8192;                  // backward: longest row whose sums over the rows are
 
-// How a thread's eight elements of a piece lie in the row.
-enum { kWide = 0, kStrided = 1, kChunk = 2 };              // 16-byte accesses; 32 apart; neighbours, element by element
+// How a thread's eight elements of a piece lie in the row: in 16-byte accesses (kWide: pieces that are whole or empty; kFull: none
+// is empty, so no branch is left in a row); 32 apart; neighbours, taken element by element.
+enum { kWide = 0, kStrided = 1, kChunk = 2, kFull = 3 };
+__host__ __device__ constexpr bool is_wide(int map) { return map == kWide || map == kFull; }
 
-// First element of piece i for a thread; the others follow at distance 1 (kWide, kChunk) or 32 (kStrided).
+// First element of piece i for a thread; the others follow at distance 1, or 32 (kStrided).
 template <int TPR, int MAP> __device__ __forceinline__ int64_t piece_at(int i, int t)
 {
     if constexpr (MAP == kStrided) return (int64_t)(i * (TPR / 32) + (t >> 5)) * 256 + (t & 31);
@@ -64,40 +66,56 @@ template <int DT> __device__ __forceinline__ void fetch_row(unsigned char *slot,
         }
     }
 }
+// A row that starts on 16 bytes and consists of whole granules.
+template <int TPR> __device__ __forceinline__ void fetch_wide(unsigned char *slot, const char *row, int bytes, int thread)
+{
+    const uint32_t dst = smem_address(slot);
+#pragma unroll 4
+    for (int at = thread * 16; at < bytes; at += TPR * 16) copy_async16(dst + at, row + at);
+}
+template <int DT, int TPR, int MAP> __device__ __forceinline__ void fetch(unsigned char *slot, const void *base, int64_t row, int64_t rows,
+                                                                          int64_t cols, int64_t ld, int thread)
+{
+    if constexpr (is_wide(MAP)) fetch_wide<TPR>(slot, (const char *)base + row * ld * Elem<DT>::BYTES, (int)cols * Elem<DT>::BYTES, thread);
+    else fetch_row<DT>(slot, base, row, rows, cols, ld, thread, TPR);
+}
 __device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void fetch_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(PENDING) : "memory"); }
+
+// Whether a piece holds anything of the row.
+template <int MAP> __device__ __forceinline__ bool piece_there(int at, int cols) { return MAP == kFull || at < cols; }
 
 // Eight elements of a row in shared memory, 0 beyond its end.
 template <int DT, int MAP> __device__ __forceinline__ void load_piece(const unsigned char *row, int at, int cols, float (&v)[8])
 {
-    if (MAP == kWide && at + 8 <= cols) {
+    if constexpr (is_wide(MAP)) {
         if constexpr (DT == UQ_BF16) {
             Elem<UQ_BF16>::unpack(*(const uint4 *)(row + at * 2), v);
         } else {
             const float4 lo = *(const float4 *)(row + at * 4), hi = *(const float4 *)(row + at * 4 + 16);
             v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
         }
-        return;
-    }
+    } else {
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        const int i = at + t * piece_step<MAP>();
-        v[t] = 0.0f;
-        if (i < cols) {
-            if constexpr (DT == UQ_BF16) v[t] = __uint_as_float((uint32_t)*(const unsigned short *)(row + i * 2) << 16);
-            else v[t] = *(const float *)(row + i * 4);
+        for (int t = 0; t < 8; ++t) {
+            const int i = at + t * piece_step<MAP>();
+            v[t] = 0.0f;
+            if (i < cols) {
+                if constexpr (DT == UQ_BF16) v[t] = __uint_as_float((uint32_t)*(const unsigned short *)(row + i * 2) << 16);
+                else v[t] = *(const float *)(row + i * 4);
+            }
         }
     }
 }
 
-template <int DT, int MAP> __device__ __forceinline__ void store_piece(void *row, int64_t at, int64_t cols, const float (&v)[8])
+template <int DT, int MAP> __device__ __forceinline__ void store_piece(void *row, int at, int cols, const float (&v)[8])
 {
     if constexpr (MAP == kStrided) {
 #pragma unroll
         for (int t = 0; t < 8; ++t)
             if (at + 32 * t < cols) store1<DT>(row, at + 32 * t, v[t]);
     } else {
-        store8<DT>(row, at, (int)max((int64_t)0, min((int64_t)8, cols - at)), MAP == kWide, v);
+        store8<DT>(row, at, is_wide(MAP) ? 8 : max(0, min(8, cols - at)), is_wide(MAP), v);
     }
 }
 
@@ -237,7 +255,7 @@ template <int DT> __device__ __forceinline__ bool quantize_piece(const uq_mx &q,
 // Sets what lies beyond the row to 0.
 template <int MAP> __device__ __forceinline__ void clear_beyond(int at, int cols, float2 (&v)[4])
 {
-    if (at + 7 * piece_step<MAP>() >= cols) {
+    if (!is_wide(MAP) && at + 7 * piece_step<MAP>() >= cols) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (at + 2 * k * piece_step<MAP>() >= cols) v[k].x = 0.0f;
@@ -279,7 +297,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
     const int64_t first = (int64_t)blockIdx.x * R + threadIdx.x / TPR, step = (int64_t)gridDim.x * R;
 #pragma unroll
     for (int i = 0; i < kRing; ++i) {
-        if (first + i * step < p.rows) fetch_row<DT>(mine + i * slot, p.x, first + i * step, p.rows, p.cols, p.ld, t, TPR);
+        if (first + i * step < p.rows) fetch<DT, TPR, MAP>(mine + i * slot, p.x, first + i * step, p.rows, p.cols, p.ld, t);
         fetch_commit();
     }
     float2 gamma[NC][4], beta[NC][4];
@@ -298,34 +316,41 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
     }
     const float inv_n = 1.0f / (float)p.cols;
     bool bad = false;
+    char *yr = (char *)p.y + first * p.y_ld * Elem<DT>::BYTES;
     fetch_wait<kRing - 1>();
     if constexpr (TPR > 32) __syncthreads(); else __syncwarp();
     int s = 0;
-    for (int64_t row = first; row < p.rows; row += step) {
-        const unsigned char *xr = mine + s * slot + (((uintptr_t)p.x + row * p.ld * Elem<DT>::BYTES) & 15);
+    for (int64_t row = first; row < p.rows; row += step, yr += step * p.y_ld * Elem<DT>::BYTES) {
+        const unsigned char *xr = mine + s * slot + (is_wide(MAP) ? 0 : ((uintptr_t)p.x + row * p.ld * Elem<DT>::BYTES) & 15);
         float2 v[NC][4], sum = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            float w[8];
-            load_piece<DT, MAP>(xr, (int)piece_at<TPR, MAP>(i, t), cols, w);
-            to_pairs(w, v[i]);
+            const int at = (int)piece_at<TPR, MAP>(i, t);
+            if (piece_there<MAP>(at, cols)) {
+                float w[8];
+                load_piece<DT, MAP>(xr, at, cols, w);
+                to_pairs(w, v[i]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum = sum + v[i][k];
+                for (int k = 0; k < 4; ++k) sum = sum + v[i][k];
+            }
         }
         fetch_wait<kRing - 2>();                           // the next row; the sum's barrier shows it to all, and frees this row's slot
         if constexpr (TPR == 32) __syncwarp();
         const float mean = row_sum<TPR>(sum.x + sum.y, scratch[0]) * inv_n;
-        if (row + kRing * step < p.rows) fetch_row<DT>(mine + s * slot, p.x, row + kRing * step, p.rows, p.cols, p.ld, t, TPR);
+        if (row + kRing * step < p.rows) fetch<DT, TPR, MAP>(mine + s * slot, p.x, row + kRing * step, p.rows, p.cols, p.ld, t);
         fetch_commit();
         s = s + 1 == kRing ? 0 : s + 1;
         sum = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
+            const int at = (int)piece_at<TPR, MAP>(i, t);
+            if (piece_there<MAP>(at, cols)) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[i][k] = v[i][k] + both(-mean);
-            clear_beyond<MAP>((int)piece_at<TPR, MAP>(i, t), cols, v[i]);
+                for (int k = 0; k < 4; ++k) v[i][k] = v[i][k] + both(-mean);
+                clear_beyond<MAP>(at, cols, v[i]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum = fma2(v[i][k], v[i][k], sum);
+                for (int k = 0; k < 4; ++k) sum = fma2(v[i][k], v[i][k], sum);
+            }
         }
         const float rstd = inverse_root(row_sum<TPR>(sum.x + sum.y, scratch[1]) * inv_n + p.eps);
         if (t == 0) {
@@ -334,13 +359,15 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         }
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-            const int64_t at = piece_at<TPR, MAP>(i, t);
+            const int at = (int)piece_at<TPR, MAP>(i, t);
+            float w[8] = {};
+            if (piece_there<MAP>(at, cols)) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[i][k] = fma2(v[i][k] * both(rstd), gamma[i][k], beta[i][k]);
-            float w[8];
-            from_pairs(v[i], w);
-            if (p.y != nullptr) store_piece<DT, MAP>((char *)p.y + row * p.y_ld * Elem<DT>::BYTES, at, p.cols, w);
-            if constexpr (MAP != kStrided) {             // (elements beyond the row are 0, and so is beta there)
+                for (int k = 0; k < 4; ++k) v[i][k] = fma2(v[i][k] * both(rstd), gamma[i][k], beta[i][k]);
+                from_pairs(v[i], w);
+                if (p.y != nullptr) store_piece<DT, MAP>(yr, at, cols, w);
+            }
+            if constexpr (MAP != kStrided) {               // (elements beyond the row are 0, and so is beta there)
                 if (p.q.codes != nullptr) bad = quantize_piece<DT>(p.q, row, at, w) || bad;
             }
         }
@@ -439,63 +466,72 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
 #pragma unroll
     for (int i = 0; i < kRing; ++i) {
         if (first + i * step < p.rows) {
-            fetch_row<DT>(mine + 2 * i * slot, p.x, first + i * step, p.rows, p.cols, p.x_ld, t, TPR);
-            fetch_row<DT>(mine + (2 * i + 1) * slot, p.dy, first + i * step, p.rows, p.cols, p.dy_ld, t, TPR);
+            fetch<DT, TPR, MAP>(mine + 2 * i * slot, p.x, first + i * step, p.rows, p.cols, p.x_ld, t);
+            fetch<DT, TPR, MAP>(mine + (2 * i + 1) * slot, p.dy, first + i * step, p.rows, p.cols, p.dy_ld, t);
         }
         fetch_commit();
     }
     const float inv_n = 1.0f / (float)p.cols;
-    const bool wide_g = ((uintptr_t)p.gamma & 15) == 0;
-    float2 dg[NC][4], db[NC][4];
+    float2 gamma[NC][4], dg[NC][4], db[NC][4];
 #pragma unroll
-    for (int i = 0; i < NC; ++i)
+    for (int i = 0; i < NC; ++i) {
+        float w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+        if (p.gamma != nullptr) load_weights<MAP>(p.gamma, piece_at<TPR, MAP>(i, t), p.cols, ((uintptr_t)p.gamma & 15) == 0, w);
+        to_pairs(w, gamma[i]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) dg[i][k] = db[i][k] = both(0.0f);
+    }
+    char *dxr = (char *)p.dx + first * p.dx_ld * Elem<DT>::BYTES;
     fetch_wait<kRing - 1>();
     if constexpr (TPR > 32) __syncthreads(); else __syncwarp();
     int s = 0, turn = 0;
-    for (int64_t row = first; row < p.rows; row += step, turn ^= 1) {
+    for (int64_t row = first; row < p.rows; row += step, turn ^= 1, dxr += step * p.dx_ld * Elem<DT>::BYTES) {
         const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
-        const unsigned char *xr = mine + 2 * s * slot + (((uintptr_t)p.x + row * p.x_ld * Elem<DT>::BYTES) & 15);
-        const unsigned char *dr = mine + (2 * s + 1) * slot + (((uintptr_t)p.dy + row * p.dy_ld * Elem<DT>::BYTES) & 15);
+        const unsigned char *xr = mine + 2 * s * slot + (is_wide(MAP) ? 0 : ((uintptr_t)p.x + row * p.x_ld * Elem<DT>::BYTES) & 15);
+        const unsigned char *dr = mine + (2 * s + 1) * slot + (is_wide(MAP) ? 0 : ((uintptr_t)p.dy + row * p.dy_ld * Elem<DT>::BYTES) & 15);
         float2 d[NC][4], xh[NC][4], sum1 = both(0.0f), sum2 = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NC; ++i) {                     // beyond the row x and dy are 0: nothing is added
             const int at = (int)piece_at<TPR, MAP>(i, t);
-            float w[8];
-            float2 g[4];
-            load_piece<DT, MAP>(xr, at, cols, w);
-            to_pairs(w, xh[i]);
-            load_piece<DT, MAP>(dr, at, cols, w);
-            to_pairs(w, d[i]);
-            if (p.gamma != nullptr) { load_weights<MAP>(p.gamma, at, p.cols, wide_g, w); to_pairs(w, g); }
+            if (piece_there<MAP>(at, cols)) {
+                float w[8];
+                load_piece<DT, MAP>(xr, at, cols, w);
+                to_pairs(w, xh[i]);
+                load_piece<DT, MAP>(dr, at, cols, w);
+                to_pairs(w, d[i]);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                xh[i][k] = (xh[i][k] + both(-mean)) * both(rstd);
-                dg[i][k] = fma2(d[i][k], xh[i][k], dg[i][k]);
-                db[i][k] = db[i][k] + d[i][k];
-                if (p.gamma != nullptr) d[i][k] = d[i][k] * g[k];
-                sum1 = sum1 + d[i][k];
-                sum2 = fma2(d[i][k], xh[i][k], sum2);
+                for (int k = 0; k < 4; ++k) {
+                    xh[i][k] = (xh[i][k] + both(-mean)) * both(rstd);
+                    dg[i][k] = fma2(d[i][k], xh[i][k], dg[i][k]);
+                    db[i][k] = db[i][k] + d[i][k];
+                    d[i][k] = d[i][k] * gamma[i][k];
+                    sum1 = sum1 + d[i][k];
+                    sum2 = fma2(d[i][k], xh[i][k], sum2);
+                }
             }
         }
         fetch_wait<kRing - 2>();                           // the next row; the barrier shows it to all, and frees this row's slot
         if constexpr (TPR == 32) __syncwarp();
         const float2 m = row_sums<TPR>(make_float2(sum1.x + sum1.y, sum2.x + sum2.y), scratch[turn]) * both(inv_n);
         if (row + kRing * step < p.rows) {
-            fetch_row<DT>(mine + 2 * s * slot, p.x, row + kRing * step, p.rows, p.cols, p.x_ld, t, TPR);
-            fetch_row<DT>(mine + (2 * s + 1) * slot, p.dy, row + kRing * step, p.rows, p.cols, p.dy_ld, t, TPR);
+            fetch<DT, TPR, MAP>(mine + 2 * s * slot, p.x, row + kRing * step, p.rows, p.cols, p.x_ld, t);
+            fetch<DT, TPR, MAP>(mine + (2 * s + 1) * slot, p.dy, row + kRing * step, p.rows, p.cols, p.dy_ld, t);
         }
         fetch_commit();
         s = s + 1 == kRing ? 0 : s + 1;
         if (p.dx != nullptr) {
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-                float w[8];
+                const int at = (int)piece_at<TPR, MAP>(i, t);
+                if (piece_there<MAP>(at, cols)) {
+                    float w[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) d[i][k] = both(rstd) * fma2(xh[i][k], both(-m.y), d[i][k] + both(-m.x));
-                from_pairs(d[i], w);
-                store_piece<DT, MAP>((char *)p.dx + row * p.dx_ld * Elem<DT>::BYTES, piece_at<TPR, MAP>(i, t), p.cols, w);
+                    for (int k = 0; k < 4; ++k) d[i][k] = both(rstd) * fma2(xh[i][k], both(-m.y), d[i][k] + both(-m.x));
+                    from_pairs(d[i], w);
+                    store_piece<DT, MAP>(dxr, at, cols, w);
+                }
             }
         }
     }
@@ -676,14 +712,15 @@ template <int DT, int TPR, int NC> void launch_forward(const NormArgs &p, int ma
     using T = RowThreads<TPR>;
     const int64_t grid = min((p.rows + T::kRows - 1) / T::kRows, (int64_t)148 * T::kResident);
     const size_t smem = (size_t)T::kRows * kRing * slot_bytes(p.cols, Elem<DT>::BYTES);
-    if (map == kWide) launch_rows(layer_norm_kernel<DT, TPR, NC, kWide>, grid, T::kThreads, smem, st, p);
+    if (map == kWide && p.cols == TPR * NC * 8) launch_rows(layer_norm_kernel<DT, TPR, NC, kFull>, grid, T::kThreads, smem, st, p);
+    else if (map == kWide) launch_rows(layer_norm_kernel<DT, TPR, NC, kWide>, grid, T::kThreads, smem, st, p);
     else if (map == kStrided) launch_rows(layer_norm_kernel<DT, TPR, NC, kStrided>, grid, T::kThreads, smem, st, p);
     else launch_rows(layer_norm_kernel<DT, TPR, NC, kChunk>, grid, T::kThreads, smem, st, p);
 }
 
 template <int DT> void launch_forward_any(const NormArgs &p, cudaStream_t st)
 {
-    const bool wide = rows_wide<DT>(p.x, p.ld) && (p.y == nullptr || rows_wide<DT>(p.y, p.y_ld));
+    const bool wide = (p.cols & 7) == 0 && rows_wide<DT>(p.x, p.ld) && (p.y == nullptr || rows_wide<DT>(p.y, p.y_ld));
     const int map = wide ? kWide : p.q.codes == nullptr ? kStrided : kChunk;
     if (p.cols <= 256) launch_forward<DT, 32, 1>(p, map, st);
     else if (p.cols <= 512) launch_forward<DT, 32, 2>(p, map, st);
@@ -699,13 +736,14 @@ template <int DT, int TPR, int NC> void launch_backward(const NormBackwardArgs &
 {
     using T = RowThreads<TPR>;
     const size_t smem = (size_t)T::kRows * kRing * 2 * slot_bytes(p.cols, Elem<DT>::BYTES);
-    if (wide) launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kWide>, parts, T::kThreads, smem, st, p);
+    if (wide && p.cols == TPR * NC * 8) launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kFull>, parts, T::kThreads, smem, st, p);
+    else if (wide) launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kWide>, parts, T::kThreads, smem, st, p);
     else launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kStrided>, parts, T::kThreads, smem, st, p);
 }
 
 template <int DT> void launch_backward_any(const NormBackwardArgs &p, int parts, bool sums, cudaStream_t st)
 {
-    const bool wide = rows_wide<DT>(p.dy, p.dy_ld) && rows_wide<DT>(p.x, p.x_ld) && (p.dx == nullptr || rows_wide<DT>(p.dx, p.dx_ld));
+    const bool wide = (p.cols & 7) == 0 && rows_wide<DT>(p.dy, p.dy_ld) && rows_wide<DT>(p.x, p.x_ld) && (p.dx == nullptr || rows_wide<DT>(p.dx, p.dx_ld));
     if (p.cols <= 256) launch_backward<DT, 32, 1>(p, wide, parts, st);
     else if (p.cols <= 512) launch_backward<DT, 32, 2>(p, wide, parts, st);
     else if (p.cols <= 1024) launch_backward<DT, 64, 2>(p, wide, parts, st);
