@@ -10,8 +10,8 @@
 // memory meanwhile, and a row is read from there once and kept in registers over its reductions, as are the weights and, in
 // the backward pass, the sums over the rows.  Rows may start anywhere: the ring takes whole 16-byte granules of memory, what
 // lies beside the row (but inside the matrix) included, and a row keeps its offset from 16 bytes there.  Which elements a
-// thread holds depends on that offset: eight neighbours in one 16-byte access, or eight that are 32 apart, so that a warp's
-// scalar accesses are contiguous.
+// thread holds depends on that offset: neighbours in 16-byte accesses, or elements that are 32 apart, so that a warp's scalar
+// accesses are contiguous.
 #include "uq_mx.cuh"
 
 namespace uq {
@@ -27,11 +27,15 @@ constexpr int64_t kLnBackwardCols = 8192;                  // backward: longest 
 enum { kWide = 0, kStrided = 1, kChunk = 2, kFull = 3 };
 __host__ __device__ constexpr bool is_wide(int map) { return map == kWide || map == kFull; }
 
-// First element of piece i for a thread; the others follow at distance 1, or 32 (kStrided).
-template <int TPR, int MAP> __device__ __forceinline__ int64_t piece_at(int i, int t)
+// Elements of a piece: what 16 bytes hold, so that a warp's accesses of either memory are contiguous; eight (a quarter of a block)
+// where the result is quantized.
+template <int DT, bool Q> constexpr int kPiece = Q ? 8 : 16 / Elem<DT>::BYTES;
+
+// First element of a thread's piece i of PE elements; the others follow at distance 1, or 32 (kStrided).
+template <int TPR, int MAP, int PE> __device__ __forceinline__ int piece_at(int i, int t)
 {
-    if constexpr (MAP == kStrided) return (int64_t)(i * (TPR / 32) + (t >> 5)) * 256 + (t & 31);
-    return (int64_t)(i * TPR + t) * 8;
+    if constexpr (MAP == kStrided) return (i * (TPR / 32) + (t >> 5)) * (PE * 32) + (t & 31);
+    return (i * TPR + t) * PE;
 }
 template <int MAP> __device__ __forceinline__ int piece_step() { return MAP == kStrided ? 32 : 1; }
 
@@ -85,19 +89,20 @@ template <int PENDING> __device__ __forceinline__ void fetch_wait() { asm volati
 // Whether a piece holds anything of the row.
 template <int MAP> __device__ __forceinline__ bool piece_there(int at, int cols) { return MAP == kFull || at < cols; }
 
-// Eight elements of a row in shared memory, 0 beyond its end.
-template <int DT, int MAP> __device__ __forceinline__ void load_piece(const unsigned char *row, int at, int cols, float (&v)[8])
+// A piece of a row in shared memory, 0 beyond its end.
+template <int DT, int MAP, int PE> __device__ __forceinline__ void load_piece(const unsigned char *row, int at, int cols, float (&v)[PE])
 {
-    if constexpr (is_wide(MAP)) {
-        if constexpr (DT == UQ_BF16) {
-            Elem<UQ_BF16>::unpack(*(const uint4 *)(row + at * 2), v);
-        } else {
-            const float4 lo = *(const float4 *)(row + at * 4), hi = *(const float4 *)(row + at * 4 + 16);
-            v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+    if constexpr (is_wide(MAP) && DT == UQ_BF16) {
+        Elem<UQ_BF16>::unpack(*(const uint4 *)(row + at * 2), v);
+    } else if constexpr (is_wide(MAP)) {
+#pragma unroll
+        for (int t = 0; t < PE; t += 4) {
+            const float4 q = *(const float4 *)(row + (at + t) * 4);
+            v[t] = q.x; v[t + 1] = q.y; v[t + 2] = q.z; v[t + 3] = q.w;
         }
     } else {
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
+        for (int t = 0; t < PE; ++t) {
             const int i = at + t * piece_step<MAP>();
             v[t] = 0.0f;
             if (i < cols) {
@@ -108,27 +113,32 @@ template <int DT, int MAP> __device__ __forceinline__ void load_piece(const unsi
     }
 }
 
-template <int DT, int MAP> __device__ __forceinline__ void store_piece(void *row, int at, int cols, const float (&v)[8])
+template <int DT, int MAP, int PE> __device__ __forceinline__ void store_piece(void *row, int at, int cols, const float (&v)[PE])
 {
-    if constexpr (MAP == kStrided) {
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-            if (at + 32 * t < cols) store1<DT>(row, at + 32 * t, v[t]);
+    if constexpr (is_wide(MAP) && PE == 4) {
+        *(float4 *)((float *)row + at) = make_float4(v[0], v[1], v[2], v[3]);
+    } else if constexpr (is_wide(MAP)) {
+        store8<DT>(row, at, 8, true, v);
     } else {
-        store8<DT>(row, at, is_wide(MAP) ? 8 : max(0, min(8, cols - at)), is_wide(MAP), v);
+#pragma unroll
+        for (int t = 0; t < PE; ++t)
+            if (at + t * piece_step<MAP>() < cols) store1<DT>(row, at + t * piece_step<MAP>(), v[t]);
     }
 }
 
-// Eight weights, cached: every row reads them.
-template <int MAP> __device__ __forceinline__ void load_weights(const float *w, int64_t at, int64_t cols, bool wide, float (&v)[8])
+// The weights of a piece, cached: every row uses them.
+template <int MAP, int PE> __device__ __forceinline__ void load_weights(const float *w, int64_t at, int64_t cols, bool wide, float (&v)[PE])
 {
-    if (MAP != kStrided && wide && at + 8 <= cols) {
-        const float4 lo = __ldg((const float4 *)(w + at)), hi = __ldg((const float4 *)(w + at + 4));
-        v[0] = lo.x; v[1] = lo.y; v[2] = lo.z; v[3] = lo.w; v[4] = hi.x; v[5] = hi.y; v[6] = hi.z; v[7] = hi.w;
+    if (MAP != kStrided && wide && at + PE <= cols) {
+#pragma unroll
+        for (int t = 0; t < PE; t += 4) {
+            const float4 q = __ldg((const float4 *)(w + at + t));
+            v[t] = q.x; v[t + 1] = q.y; v[t + 2] = q.z; v[t + 3] = q.w;
+        }
         return;
     }
 #pragma unroll
-    for (int t = 0; t < 8; ++t) v[t] = at + t * piece_step<MAP>() < cols ? __ldg(w + at + t * piece_step<MAP>()) : 0.0f;
+    for (int t = 0; t < PE; ++t) v[t] = at + t * piece_step<MAP>() < cols ? __ldg(w + at + t * piece_step<MAP>()) : 0.0f;
 }
 
 // Two values per instruction: the row's elements are held in pairs.
@@ -163,15 +173,15 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
     return pair_of(r);
 }
 __device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-__device__ __forceinline__ void to_pairs(const float (&v)[8], float2 (&w)[4])
+template <int PE> __device__ __forceinline__ void to_pairs(const float (&v)[PE], float2 (&w)[PE / 2])
 {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = make_float2(v[2 * k], v[2 * k + 1]);
+    for (int k = 0; k < PE / 2; ++k) w[k] = make_float2(v[2 * k], v[2 * k + 1]);
 }
-__device__ __forceinline__ void from_pairs(const float2 (&w)[4], float (&v)[8])
+template <int PE> __device__ __forceinline__ void from_pairs(const float2 (&w)[PE / 2], float (&v)[PE])
 {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { v[2 * k] = w[k].x; v[2 * k + 1] = w[k].y; }
+    for (int k = 0; k < PE / 2; ++k) { v[2 * k] = w[k].x; v[2 * k + 1] = w[k].y; }
 }
 
 __device__ __forceinline__ float warp_sum(float v)
@@ -253,11 +263,11 @@ template <int DT> __device__ __forceinline__ bool quantize_piece(const uq_mx &q,
 }
 
 // Sets what lies beyond the row to 0.
-template <int MAP> __device__ __forceinline__ void clear_beyond(int at, int cols, float2 (&v)[4])
+template <int MAP, int PE> __device__ __forceinline__ void clear_beyond(int at, int cols, float2 (&v)[PE / 2])
 {
-    if (!is_wide(MAP) && at + 7 * piece_step<MAP>() >= cols) {
+    if (!is_wide(MAP) && at + (PE - 1) * piece_step<MAP>() >= cols) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < PE / 2; ++k) {
             if (at + 2 * k * piece_step<MAP>() >= cols) v[k].x = 0.0f;
             if (at + (2 * k + 1) * piece_step<MAP>() >= cols) v[k].y = 0.0f;
         }
@@ -284,10 +294,10 @@ template <int TPR> struct RowThreads {
     static constexpr int kResident = 512 / kThreads;
 };
 
-template <int DT, int TPR, int NC, int MAP>
+template <int DT, int TPR, int NC, int MAP, bool Q>
 __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kResident) layer_norm_kernel(const NormArgs p)
 {
-    constexpr int R = RowThreads<TPR>::kRows;
+    constexpr int R = RowThreads<TPR>::kRows, PE = kPiece<DT, Q>, NP = NC * 8 / PE;
     __shared__ __align__(16) float scratch[2][TPR / 32];
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_prologue();
@@ -300,19 +310,19 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         if (first + i * step < p.rows) fetch<DT, TPR, MAP>(mine + i * slot, p.x, first + i * step, p.rows, p.cols, p.ld, t);
         fetch_commit();
     }
-    float2 gamma[NC][4], beta[NC][4];
+    float2 gamma[NP][PE / 2], beta[NP][PE / 2];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        const int64_t at = piece_at<TPR, MAP>(i, t);
-        float w[8];
+    for (int i = 0; i < NP; ++i) {
+        const int at = piece_at<TPR, MAP, PE>(i, t);
+        float w[PE];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = 1.0f;
-        if (p.gamma != nullptr) load_weights<MAP>(p.gamma, at, p.cols, ((uintptr_t)p.gamma & 15) == 0, w);
-        to_pairs(w, gamma[i]);
+        for (int k = 0; k < PE; ++k) w[k] = 1.0f;
+        if (p.gamma != nullptr) load_weights<MAP, PE>(p.gamma, at, p.cols, ((uintptr_t)p.gamma & 15) == 0, w);
+        to_pairs<PE>(w, gamma[i]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = 0.0f;
-        if (p.beta != nullptr) load_weights<MAP>(p.beta, at, p.cols, ((uintptr_t)p.beta & 15) == 0, w);
-        to_pairs(w, beta[i]);
+        for (int k = 0; k < PE; ++k) w[k] = 0.0f;
+        if (p.beta != nullptr) load_weights<MAP, PE>(p.beta, at, p.cols, ((uintptr_t)p.beta & 15) == 0, w);
+        to_pairs<PE>(w, beta[i]);
     }
     const float inv_n = 1.0f / (float)p.cols;
     bool bad = false;
@@ -322,16 +332,16 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
     int s = 0;
     for (int64_t row = first; row < p.rows; row += step, yr += step * p.y_ld * Elem<DT>::BYTES) {
         const unsigned char *xr = mine + s * slot + (is_wide(MAP) ? 0 : ((uintptr_t)p.x + row * p.ld * Elem<DT>::BYTES) & 15);
-        float2 v[NC][4], sum = both(0.0f);
+        float2 v[NP][PE / 2], sum = both(0.0f);
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int at = (int)piece_at<TPR, MAP>(i, t);
+        for (int i = 0; i < NP; ++i) {
+            const int at = piece_at<TPR, MAP, PE>(i, t);
             if (piece_there<MAP>(at, cols)) {
-                float w[8];
-                load_piece<DT, MAP>(xr, at, cols, w);
-                to_pairs(w, v[i]);
+                float w[PE];
+                load_piece<DT, MAP, PE>(xr, at, cols, w);
+                to_pairs<PE>(w, v[i]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum = sum + v[i][k];
+                for (int k = 0; k < PE / 2; ++k) sum = sum + v[i][k];
             }
         }
         fetch_wait<kRing - 2>();                           // the next row; the sum's barrier shows it to all, and frees this row's slot
@@ -342,14 +352,14 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         s = s + 1 == kRing ? 0 : s + 1;
         sum = both(0.0f);
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int at = (int)piece_at<TPR, MAP>(i, t);
+        for (int i = 0; i < NP; ++i) {
+            const int at = piece_at<TPR, MAP, PE>(i, t);
             if (piece_there<MAP>(at, cols)) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[i][k] = v[i][k] + both(-mean);
-                clear_beyond<MAP>(at, cols, v[i]);
+                for (int k = 0; k < PE / 2; ++k) v[i][k] = v[i][k] + both(-mean);
+                clear_beyond<MAP, PE>(at, cols, v[i]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum = fma2(v[i][k], v[i][k], sum);
+                for (int k = 0; k < PE / 2; ++k) sum = fma2(v[i][k], v[i][k], sum);
             }
         }
         const float rstd = inverse_root(row_sum<TPR>(sum.x + sum.y, scratch[1]) * inv_n + p.eps);
@@ -358,21 +368,19 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
             if (p.rstd != nullptr) p.rstd[row] = rstd;
         }
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            const int at = (int)piece_at<TPR, MAP>(i, t);
-            float w[8] = {};
+        for (int i = 0; i < NP; ++i) {
+            const int at = piece_at<TPR, MAP, PE>(i, t);
+            float w[PE] = {};
             if (piece_there<MAP>(at, cols)) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[i][k] = fma2(v[i][k] * both(rstd), gamma[i][k], beta[i][k]);
-                from_pairs(v[i], w);
-                if (p.y != nullptr) store_piece<DT, MAP>(yr, at, cols, w);
+                for (int k = 0; k < PE / 2; ++k) v[i][k] = fma2(v[i][k] * both(rstd), gamma[i][k], beta[i][k]);
+                from_pairs<PE>(v[i], w);
+                if (p.y != nullptr) store_piece<DT, MAP, PE>(yr, at, cols, w);
             }
-            if constexpr (MAP != kStrided) {               // (elements beyond the row are 0, and so is beta there)
-                if (p.q.codes != nullptr) bad = quantize_piece<DT>(p.q, row, at, w) || bad;
-            }
+            if constexpr (Q) bad = quantize_piece<DT>(p.q, row, at, w) || bad;      // (elements beyond the row are 0, and so is beta)
         }
     }
-    if (bad && p.status != nullptr) atomicOr(p.status, UQ_STATUS_NONFINITE);
+    if (Q && bad && p.status != nullptr) atomicOr(p.status, UQ_STATUS_NONFINITE);
 }
 
 // Rows of any length: read three times (the second and third time from the caches).
@@ -421,12 +429,12 @@ __global__ void __launch_bounds__(kLnThreads) layer_norm_long_kernel(const NormA
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = (v[k] - mean) * rstd;
         if (p.gamma != nullptr) {
-            load_weights<kWide>(p.gamma, c * 8, cols, wide_g, w);
+            load_weights<kWide, 8>(p.gamma, c * 8, cols, wide_g, w);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] *= w[k];
         }
         if (p.beta != nullptr) {
-            load_weights<kWide>(p.beta, c * 8, cols, wide_b, w);
+            load_weights<kWide, 8>(p.beta, c * 8, cols, wide_b, w);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] += w[k];
         }
@@ -455,7 +463,7 @@ struct NormBackwardArgs {
 template <int DT, int TPR, int NC, int MAP>
 __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kResident) layer_norm_backward_kernel(const NormBackwardArgs p)
 {
-    constexpr int R = RowThreads<TPR>::kRows, T = RowThreads<TPR>::kThreads;
+    constexpr int R = RowThreads<TPR>::kRows, T = RowThreads<TPR>::kThreads, PE = kPiece<DT, false>, NP = NC * 8 / PE;
     __shared__ __align__(16) float2 scratch[2][TPR / 32];
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_prologue();
@@ -472,37 +480,42 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         fetch_commit();
     }
     const float inv_n = 1.0f / (float)p.cols;
-    float2 gamma[NC][4], dg[NC][4], db[NC][4];
+    float2 gamma[NP][PE / 2], dg[NP][PE / 2], db[NP][PE / 2];
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-        float w[8];
+    for (int i = 0; i < NP; ++i) {
+        float w[PE];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = 1.0f;
-        if (p.gamma != nullptr) load_weights<MAP>(p.gamma, piece_at<TPR, MAP>(i, t), p.cols, ((uintptr_t)p.gamma & 15) == 0, w);
-        to_pairs(w, gamma[i]);
+        for (int k = 0; k < PE; ++k) w[k] = 1.0f;
+        if (p.gamma != nullptr) load_weights<MAP, PE>(p.gamma, piece_at<TPR, MAP, PE>(i, t), p.cols, ((uintptr_t)p.gamma & 15) == 0, w);
+        to_pairs<PE>(w, gamma[i]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) dg[i][k] = db[i][k] = both(0.0f);
+        for (int k = 0; k < PE / 2; ++k) dg[i][k] = db[i][k] = both(0.0f);
     }
     char *dxr = (char *)p.dx + first * p.dx_ld * Elem<DT>::BYTES;
     fetch_wait<kRing - 1>();
     if constexpr (TPR > 32) __syncthreads(); else __syncwarp();
     int s = 0, turn = 0;
+    float next_mean = first < p.rows ? __ldg(p.mean + first) : 0.0f, next_rstd = first < p.rows ? __ldg(p.rstd + first) : 0.0f;
     for (int64_t row = first; row < p.rows; row += step, turn ^= 1, dxr += step * p.dx_ld * Elem<DT>::BYTES) {
-        const float mean = __ldg(p.mean + row), rstd = __ldg(p.rstd + row);
+        const float mean = next_mean, rstd = next_rstd;    // (loaded a row ahead: nothing else in a row waits for memory)
+        if (row + step < p.rows) {
+            next_mean = __ldg(p.mean + row + step);
+            next_rstd = __ldg(p.rstd + row + step);
+        }
         const unsigned char *xr = mine + 2 * s * slot + (is_wide(MAP) ? 0 : ((uintptr_t)p.x + row * p.x_ld * Elem<DT>::BYTES) & 15);
         const unsigned char *dr = mine + (2 * s + 1) * slot + (is_wide(MAP) ? 0 : ((uintptr_t)p.dy + row * p.dy_ld * Elem<DT>::BYTES) & 15);
-        float2 d[NC][4], xh[NC][4], sum1 = both(0.0f), sum2 = both(0.0f);
+        float2 d[NP][PE / 2], xh[NP][PE / 2], sum1 = both(0.0f), sum2 = both(0.0f);
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {                     // beyond the row x and dy are 0: nothing is added
-            const int at = (int)piece_at<TPR, MAP>(i, t);
+        for (int i = 0; i < NP; ++i) {                     // beyond the row x and dy are 0: nothing is added
+            const int at = piece_at<TPR, MAP, PE>(i, t);
             if (piece_there<MAP>(at, cols)) {
-                float w[8];
-                load_piece<DT, MAP>(xr, at, cols, w);
-                to_pairs(w, xh[i]);
-                load_piece<DT, MAP>(dr, at, cols, w);
-                to_pairs(w, d[i]);
+                float w[PE];
+                load_piece<DT, MAP, PE>(xr, at, cols, w);
+                to_pairs<PE>(w, xh[i]);
+                load_piece<DT, MAP, PE>(dr, at, cols, w);
+                to_pairs<PE>(w, d[i]);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < PE / 2; ++k) {
                     xh[i][k] = (xh[i][k] + both(-mean)) * both(rstd);
                     dg[i][k] = fma2(d[i][k], xh[i][k], dg[i][k]);
                     db[i][k] = db[i][k] + d[i][k];
@@ -523,14 +536,14 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         s = s + 1 == kRing ? 0 : s + 1;
         if (p.dx != nullptr) {
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                const int at = (int)piece_at<TPR, MAP>(i, t);
+            for (int i = 0; i < NP; ++i) {
+                const int at = piece_at<TPR, MAP, PE>(i, t);
                 if (piece_there<MAP>(at, cols)) {
-                    float w[8];
+                    float w[PE];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) d[i][k] = both(rstd) * fma2(xh[i][k], both(-m.y), d[i][k] + both(-m.x));
-                    from_pairs(d[i], w);
-                    store_piece<DT, MAP>(dxr, at, cols, w);
+                    for (int k = 0; k < PE / 2; ++k) d[i][k] = both(rstd) * fma2(xh[i][k], both(-m.y), d[i][k] + both(-m.x));
+                    from_pairs<PE>(d[i], w);
+                    store_piece<DT, MAP, PE>(dxr, at, cols, w);
                 }
             }
         }
@@ -542,13 +555,13 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         for (int w = 0; w < R; ++w) {
             if (part == w) {
 #pragma unroll
-                for (int i = 0; i < NC; ++i) {
-                    float g[8], b[8];
-                    from_pairs(dg[i], g);
-                    from_pairs(db[i], b);
+                for (int i = 0; i < NP; ++i) {
+                    float g[PE], b[PE];
+                    from_pairs<PE>(dg[i], g);
+                    from_pairs<PE>(db[i], b);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int c = (int)piece_at<TPR, MAP>(i, t) + k * piece_step<MAP>();
+                    for (int k = 0; k < PE; ++k) {
+                        const int c = piece_at<TPR, MAP, PE>(i, t) + k * piece_step<MAP>();
                         if (c < cols) {
                             sums[c] = w == 0 ? g[k] : sums[c] + g[k];
                             sums[cols + c] = w == 0 ? b[k] : sums[cols + c] + b[k];
@@ -561,13 +574,13 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         for (int c = threadIdx.x; c < 2 * cols; c += T) out[c] = sums[c];
     } else {
 #pragma unroll
-        for (int i = 0; i < NC; ++i) {
-            float g[8], b[8];
-            from_pairs(dg[i], g);
-            from_pairs(db[i], b);
+        for (int i = 0; i < NP; ++i) {
+            float g[PE], b[PE];
+            from_pairs<PE>(dg[i], g);
+            from_pairs<PE>(db[i], b);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int c = (int)piece_at<TPR, MAP>(i, t) + k * piece_step<MAP>();
+            for (int k = 0; k < PE; ++k) {
+                const int c = piece_at<TPR, MAP, PE>(i, t) + k * piece_step<MAP>();
                 if (c < cols) { out[c] = g[k]; out[cols + c] = b[k]; }
             }
         }
@@ -595,7 +608,7 @@ __global__ void __launch_bounds__(kLnThreads) layer_norm_backward_long_kernel(co
         float d[8], v[8], w[8];
         load8<DT>(dr, c * 8, have, wide_dy, d);
         load8<DT>(xr, c * 8, have, wide_x, v);
-        if (p.gamma != nullptr) load_weights<kWide>(p.gamma, c * 8, cols, wide_g, w);
+        if (p.gamma != nullptr) load_weights<kWide, 8>(p.gamma, c * 8, cols, wide_g, w);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             if (k < have) {
@@ -611,7 +624,7 @@ __global__ void __launch_bounds__(kLnThreads) layer_norm_backward_long_kernel(co
         float d[8], v[8], w[8];
         load8<DT>(dr, c * 8, have, wide_dy, d);
         load8<DT>(xr, c * 8, have, wide_x, v);
-        if (p.gamma != nullptr) load_weights<kWide>(p.gamma, c * 8, cols, wide_g, w);
+        if (p.gamma != nullptr) load_weights<kWide, 8>(p.gamma, c * 8, cols, wide_g, w);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const float g = p.gamma != nullptr ? d[k] * w[k] : d[k];
@@ -707,28 +720,34 @@ template <typename K, typename A> void launch_rows(K *kernel, int64_t grid, int 
     launch_k_smem(kernel, dim3((unsigned)grid), dim3(threads), smem, st, args);
 }
 
-template <int DT, int TPR, int NC> void launch_forward(const NormArgs &p, int map, cudaStream_t st)
+template <int DT, int TPR, int NC> void launch_forward(const NormArgs &p, bool wide, cudaStream_t st)
 {
     using T = RowThreads<TPR>;
     const int64_t grid = min((p.rows + T::kRows - 1) / T::kRows, (int64_t)148 * T::kResident);
     const size_t smem = (size_t)T::kRows * kRing * slot_bytes(p.cols, Elem<DT>::BYTES);
-    if (map == kWide && p.cols == TPR * NC * 8) launch_rows(layer_norm_kernel<DT, TPR, NC, kFull>, grid, T::kThreads, smem, st, p);
-    else if (map == kWide) launch_rows(layer_norm_kernel<DT, TPR, NC, kWide>, grid, T::kThreads, smem, st, p);
-    else if (map == kStrided) launch_rows(layer_norm_kernel<DT, TPR, NC, kStrided>, grid, T::kThreads, smem, st, p);
-    else launch_rows(layer_norm_kernel<DT, TPR, NC, kChunk>, grid, T::kThreads, smem, st, p);
+    const bool full = p.cols == TPR * NC * 8;
+    if (p.q.codes != nullptr) {
+        if (!wide) launch_rows(layer_norm_kernel<DT, TPR, NC, kChunk, true>, grid, T::kThreads, smem, st, p);
+        else if (full) launch_rows(layer_norm_kernel<DT, TPR, NC, kFull, true>, grid, T::kThreads, smem, st, p);
+        else launch_rows(layer_norm_kernel<DT, TPR, NC, kWide, true>, grid, T::kThreads, smem, st, p);
+    } else {
+        if (!wide) launch_rows(layer_norm_kernel<DT, TPR, NC, kStrided, false>, grid, T::kThreads, smem, st, p);
+        else if (full) launch_rows(layer_norm_kernel<DT, TPR, NC, kFull, false>, grid, T::kThreads, smem, st, p);
+        else launch_rows(layer_norm_kernel<DT, TPR, NC, kWide, false>, grid, T::kThreads, smem, st, p);
+    }
 }
 
 template <int DT> void launch_forward_any(const NormArgs &p, cudaStream_t st)
 {
-    const bool wide = (p.cols & 7) == 0 && rows_wide<DT>(p.x, p.ld) && (p.y == nullptr || rows_wide<DT>(p.y, p.y_ld));
-    const int map = wide ? kWide : p.q.codes == nullptr ? kStrided : kChunk;
-    if (p.cols <= 256) launch_forward<DT, 32, 1>(p, map, st);
-    else if (p.cols <= 512) launch_forward<DT, 32, 2>(p, map, st);
-    else if (p.cols <= 1024) launch_forward<DT, 64, 2>(p, map, st);
-    else if (p.cols <= 2048) launch_forward<DT, 128, 2>(p, map, st);
-    else if (p.cols <= 4096) launch_forward<DT, 128, 4>(p, map, st);
-    else if (p.cols <= 8192) launch_forward<DT, 256, 4>(p, map, st);
-    else if (p.cols <= kLnRegisterCols) launch_forward<DT, 512, 4>(p, map, st);
+    const int piece = p.q.codes != nullptr ? 8 : 16 / Elem<DT>::BYTES;
+    const bool wide = p.cols % piece == 0 && rows_wide<DT>(p.x, p.ld) && (p.y == nullptr || rows_wide<DT>(p.y, p.y_ld));
+    if (p.cols <= 256) launch_forward<DT, 32, 1>(p, wide, st);
+    else if (p.cols <= 512) launch_forward<DT, 32, 2>(p, wide, st);
+    else if (p.cols <= 1024) launch_forward<DT, 64, 2>(p, wide, st);
+    else if (p.cols <= 2048) launch_forward<DT, 128, 2>(p, wide, st);
+    else if (p.cols <= 4096) launch_forward<DT, 128, 4>(p, wide, st);
+    else if (p.cols <= 8192) launch_forward<DT, 256, 4>(p, wide, st);
+    else if (p.cols <= kLnRegisterCols) launch_forward<DT, 512, 4>(p, wide, st);
     else launch_k(layer_norm_long_kernel<DT>, dim3((unsigned)p.rows), dim3(kLnThreads), st, p);
 }
 
@@ -743,7 +762,7 @@ template <int DT, int TPR, int NC> void launch_backward(const NormBackwardArgs &
 
 template <int DT> void launch_backward_any(const NormBackwardArgs &p, int parts, bool sums, cudaStream_t st)
 {
-    const bool wide = (p.cols & 7) == 0 && rows_wide<DT>(p.dy, p.dy_ld) && rows_wide<DT>(p.x, p.x_ld) && (p.dx == nullptr || rows_wide<DT>(p.dx, p.dx_ld));
+    const bool wide = p.cols % (16 / Elem<DT>::BYTES) == 0 && rows_wide<DT>(p.dy, p.dy_ld) && rows_wide<DT>(p.x, p.x_ld) && (p.dx == nullptr || rows_wide<DT>(p.dx, p.dx_ld));
     if (p.cols <= 256) launch_backward<DT, 32, 1>(p, wide, parts, st);
     else if (p.cols <= 512) launch_backward<DT, 32, 2>(p, wide, parts, st);
     else if (p.cols <= 1024) launch_backward<DT, 64, 2>(p, wide, parts, st);
