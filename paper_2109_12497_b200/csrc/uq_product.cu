@@ -25,13 +25,33 @@ constexpr int kRows = 128;                                 // of b per tile
 constexpr int kStageK = 256;                               // columns per stage: 128 bytes of a row
 constexpr int kPThreads = 192;                             // warp 0 copies, warp 1 multiplies, warps 2 to 5 store
 
+template <int DT> __device__ __forceinline__ float load1(const void *base, int64_t at)
+{
+    if constexpr (DT == UQ_BF16) return __uint_as_float((uint32_t)((const unsigned short *)base)[at] << 16);
+    else return ((const float *)base)[at];
+}
+
 template <int DT> __device__ __forceinline__ void store_result(const ProductArgs &p, int64_t i, int64_t j, float v)
 {
-    if (p.add != nullptr) {
-        if constexpr (DT == UQ_BF16) v += __uint_as_float((uint32_t)((const unsigned short *)p.add)[i * p.add_ld + j] << 16);
-        else v += ((const float *)p.add)[i * p.add_ld + j];
-    }
+    if (p.add != nullptr) v += load1<DT>(p.add, i * p.add_ld + j);
     store1<DT>(p.out, i * p.ld + j, v);
+}
+
+// 16 rows of out from row i on, in one column: what is added is loaded first, all of it (it may be out itself, so the compiler
+// cannot move a load in front of a store).
+template <int DT> __device__ __forceinline__ void store_column(const ProductArgs &p, int64_t i, int64_t j, float (&v)[16])
+{
+    const int have = (int)min((int64_t)16, p.m - i);
+    if (p.add != nullptr) {
+        float w[16];
+#pragma unroll
+        for (int t = 0; t < 16; ++t) w[t] = t < have ? load1<DT>(p.add, (i + t) * p.add_ld + j) : 0.0f;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) v[t] += w[t];
+    }
+#pragma unroll
+    for (int t = 0; t < 16; ++t)
+        if (t < have) store1<DT>(p.out, (i + t) * p.ld + j, v[t]);
 }
 
 template <int NT> struct ProductShape {
@@ -74,7 +94,7 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
         barrier_init_visible();
     }
     grid_dependency_wait();                                // tensor memory too is taken only after the kernel in front has given its back
-    if (warp == 1) tmem_alloc(smem_address(tmem_slot), S::kColumns);
+    if (warp == 1) tmem_alloc<1>(smem_address(tmem_slot), S::kColumns);
     tensor_fence_before();
     __syncthreads();
     tensor_fence_after();
@@ -105,18 +125,18 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
 #pragma unroll
             for (int h = 0; h < 2; ++h) {                  // a scale tile: 128 columns
                 if (left > 128 * h) {
-                    tmem_copy_scales(sb + 4 * h, scales_descriptor(scales + 512 * h));
-                    tmem_copy_scales(sa + 4 * h, scales_descriptor(scales + 1024 + 512 * h));
+                    tmem_copy_scales<1>(sb + 4 * h, scales_descriptor(scales + 512 * h));
+                    tmem_copy_scales<1>(sa + 4 * h, scales_descriptor(scales + 1024 + 512 * h));
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
                         if (left > 128 * h + 64 * q)
-                            mma_mxf4(tmem, db + (2 * h + q) * 2, da + (2 * h + q) * 2, mxf4_instruction(kRows, NT, q), sb + 4 * h, sa + 4 * h,
+                            mma_mxf4<1>(tmem, db + (2 * h + q) * 2, da + (2 * h + q) * 2, mxf4_instruction(kRows, NT, q), sb + 4 * h, sa + 4 * h,
                                      i > s0 || h > 0 || q > 0);
                 }
             }
-            tensor_commit(empty + 8 * s);
+            tensor_commit<1>(empty + 8 * s);
         }
-        tensor_commit(done);
+        tensor_commit<1>(done);
         int again = 0;                                     // (a wait of its own: tensor memory is given back only when nothing writes it)
         if (!barrier_wait(done, 0, &again)) *gave_up = 1;
     }
@@ -131,6 +151,7 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
 #pragma unroll 1
         for (int c = 0; c < NT; c += 16) {
             float v[16];
+            __syncwarp();
             tmem_load16(acc + c, v);
             tmem_load_wait();
             if (p.split > 1) {
@@ -138,10 +159,7 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
 #pragma unroll
                 for (int t = 0; t < 16; ++t) sums[(c + t) * kRows + quarter * 32 + lane] = v[t];
             } else if (j < p.n) {
-                const int have = (int)min((int64_t)16, p.m - m0 - c);
-#pragma unroll
-                for (int t = 0; t < 16; ++t)
-                    if (t < have) store_result<DT>(p, m0 + c + t, j, v[t]);
+                store_column<DT>(p, m0 + c, j, v);
             }
         }
         tensor_fence_before();
@@ -159,7 +177,7 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
     __syncwarp();
     if (warp == 1) {
         tensor_fence_after();
-        tmem_free(tmem, S::kColumns);
+        tmem_free<1>(tmem, S::kColumns);
     }
     if (p.split > 1) {
         cluster_sync();
@@ -171,6 +189,181 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
             if (m0 + c < p.m && n0 + l < p.n) store_result<DT>(p, m0 + c, n0 + l, v);
         }
         cluster_sync();                                    // the others may still be reading here
+    }
+}
+
+// ---- large products: pairs of CTAs ----------------------------------------------------------------
+//
+// A pair of CTAs multiplies 256 rows of b (128 in either CTA's tensor memory) by NT of a: each fetches its 128 rows of b, half of
+// a's rows, and the scales of both; the even CTA issues the multiplies for both.  Per multiply-add that is half the shared memory
+// traffic and half the reads of a single CTA's tile of 128 x 128.  The pairs stay and take one tile after another; a tile's sums
+// are stored while the next tile is multiplied.  Tensor memory holds the sums of two tiles that overlap in the columns that the
+// scales leave too few: those are stored first, and the next tile starts when they are.
+
+template <int NT> struct PairShape {
+    static constexpr int kStageBytes = kRows * 128 + NT / 2 * 128 + 1024 + (NT + 127) / 128 * 1024;
+    static constexpr int kStages = NT == 256 ? 6 : 8;
+    static constexpr int kScaleSlots = 3;                  // a slot's scales are overwritten when its multiplies are done
+    static constexpr int kSlotColumns = 2 * (4 + (NT + 127) / 128 * 4);
+    static constexpr int kScales = 512 - kScaleSlots * kSlotColumns;      // first column of the scales
+    static constexpr int kSecond = kScales - NT < NT ? (kScales - NT) / 16 * 16 : NT;   // first column of the second tile's sums
+    static constexpr int kShared = NT - kSecond;           // columns that are stored first
+    static constexpr int kSmem = kStages * kStageBytes + 1024 + 256;
+};
+
+// The tile at a place in the order of the work: groups of eight rows of tiles, so that what runs at one time shares its operands
+// in the L2 cache.
+__device__ __forceinline__ void tile_place(int64_t t, int64_t tiles_m, int64_t tiles_n, int64_t *tm, int64_t *tn)
+{
+    const int64_t group = t / (8 * tiles_n), first = group * 8, height = min((int64_t)8, tiles_m - first), in = t - group * 8 * tiles_n;
+    *tm = first + in % height;
+    *tn = in / height;
+}
+
+template <int NT, int DT>
+__global__ void __launch_bounds__(kPThreads) __cluster_dims__(2, 1, 1)
+product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                    const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb, const ProductArgs p)
+{
+    using S = PairShape<NT>;
+    constexpr int ST = S::kStages;
+    extern __shared__ unsigned char raw[];
+    unsigned char *base = (unsigned char *)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    const uint32_t data = smem_address(base);
+    uint64_t *bars = (uint64_t *)(base + ST * S::kStageBytes);
+    const uint32_t full = smem_address(bars), empty = full + 8 * ST, sums_ready = full + 16 * ST, sums_free = sums_ready + 8, drained = sums_ready + 16;
+    uint32_t *tmem_slot = (uint32_t *)(bars + 2 * ST + 3);
+    volatile int *gave_up = (volatile int *)(tmem_slot + 1);
+    volatile int *issued = gave_up + 1;
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t rank = cluster_rank();
+    const int64_t tiles_n = (p.n + 255) / 256, tiles_m = (p.m + NT - 1) / NT, tiles = tiles_m * tiles_n;
+    const int64_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int stages = (int)((p.k + kStageK - 1) / kStageK);
+
+    grid_dependency_trigger();
+    if (tid == 0) {
+        for (int s = 0; s < 2 * ST + 1; ++s) barrier_init(full + 8 * s, 1);
+        barrier_init(sums_free, 8);                        // four warps of either CTA
+        barrier_init(drained, 1);
+        *gave_up = 0;
+        *issued = 0;
+        barrier_init_visible();
+    }
+    grid_dependency_wait();
+    if (warp == 1) tmem_alloc<2>(smem_address(tmem_slot), 512);
+    tensor_fence_before();
+    __syncthreads();
+    cluster_sync();                                        // both CTAs' barriers are there
+    tensor_fence_after();
+    const uint32_t tmem = *(volatile uint32_t *)tmem_slot;
+
+    if (warp == 0 && lane == 0) {
+        const uint32_t leader_full = cluster_address(full, 0);
+        int use = 0;                                       // how many stages this CTA has filled
+        for (int64_t t = pair; t < tiles && *gave_up == 0; t += pairs) {
+            int64_t tm, tn;
+            tile_place(t, tiles_m, tiles_n, &tm, &tn);
+            const int row_b = (int)(tn * 256 + rank * 128), row_a = (int)(tm * NT + rank * (NT / 2));
+            for (int i = 0; i < stages; ++i, ++use) {
+                const int s = use % ST, round = use / ST;
+                if (round > 0 && !barrier_wait(empty + 8 * s, (round - 1) & 1, gave_up)) break;
+                const uint32_t at = data + s * S::kStageBytes, bar = leader_full + 8 * s;
+                if (rank == 0) barrier_expect(full + 8 * s, 2 * S::kStageBytes);
+                copy_tile_pair(at, &map_b, i * 128, row_b, bar);
+                copy_tile_pair(at + kRows * 128, &map_a, i * 128, row_a, bar);
+                copy_tile_pair(at + kRows * 128 + NT / 2 * 128, &map_sb, i * 256, row_b >> 7, bar);
+                copy_tile_pair(at + kRows * 128 + NT / 2 * 128 + 1024, &map_sa, i * 256, (int)(tm * NT >> 7), bar);
+                *issued = use + 1;
+            }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        int use = 0, turn = 0;
+        for (int64_t t = pair; t < tiles; t += pairs, ++turn) {
+            if (turn > 0 && !barrier_wait(sums_free, (turn - 1) & 1, gave_up)) break;
+            tensor_fence_after();
+            const uint32_t sums = tmem + (turn & 1) * S::kSecond;
+            for (int i = 0; i < stages; ++i, ++use) {
+                const int s = use % ST;
+                const int before = use - S::kScaleSlots;   // the stage whose scales are overwritten
+                if (before >= 0 && !barrier_wait(empty + 8 * (before % ST), (before / ST) & 1, gave_up)) break;
+                if (!barrier_wait(full + 8 * s, (use / ST) & 1, gave_up)) break;
+                tensor_fence_after();
+                const uint32_t at = data + s * S::kStageBytes, scales = at + kRows * 128 + NT / 2 * 128;
+                const uint32_t slot = tmem + S::kScales + (use % S::kScaleSlots) * S::kSlotColumns;
+                const uint64_t db = operand_descriptor(at), da = operand_descriptor(at + kRows * 128);
+                const int64_t left = p.k - (int64_t)i * kStageK;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (left > 128 * h) {
+                        const uint32_t sb = slot + h * (S::kSlotColumns / 2), sa = sb + 4;
+                        tmem_copy_scales<2>(sb, scales_descriptor(scales + 512 * h));
+#pragma unroll
+                        for (int w = 0; w < (NT + 127) / 128; ++w) tmem_copy_scales<2>(sa + 4 * w, scales_descriptor(scales + 1024 * (1 + w) + 512 * h));
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            if (left > 128 * h + 64 * q)
+                                mma_mxf4<2>(sums, db + (2 * h + q) * 2, da + (2 * h + q) * 2, mxf4_instruction(256, NT, q), sb, sa,
+                                            i > 0 || h > 0 || q > 0);
+                    }
+                }
+                tensor_commit<2>(empty + 8 * s);
+            }
+            if (*gave_up != 0) break;
+            tensor_commit<2>(sums_ready);
+        }
+        if (*gave_up != 0) {                               // tensor memory is given back only when nothing writes it
+            int again = 0;
+            tensor_commit<2>(drained);
+            barrier_wait(drained, 0, &again);
+        }
+    } else if (warp >= 2) {
+        const int quarter = warp & 3;
+        const uint32_t free_bar = cluster_address(sums_free, 0);
+        int turn = 0;
+        for (int64_t t = pair; t < tiles; t += pairs, ++turn) {
+            int64_t tm, tn;
+            tile_place(t, tiles_m, tiles_n, &tm, &tn);
+            if (!barrier_wait(sums_ready, turn & 1, gave_up)) break;
+            tensor_fence_after();
+            const int64_t j = tn * 256 + rank * 128 + quarter * 32 + lane, m0 = tm * NT;
+            const uint32_t sums = tmem + (turn & 1) * S::kSecond + ((uint32_t)(quarter * 32) << 16);
+            // the first of two overlapping tiles shares its last columns, the second its first
+            const int first = (turn & 1) || S::kShared == 0 ? 0 : NT - S::kShared;
+#pragma unroll 1
+            for (int done = 0; done < NT; done += 16) {
+                const int c = first + done < NT ? first + done : first + done - NT;
+                float v[16];
+                __syncwarp();
+                tmem_load16(sums + c, v);
+                tmem_load_wait();
+                if (done + 16 == (S::kShared == 0 ? NT : S::kShared)) {
+                    tensor_fence_before();
+                    __syncwarp();
+                    if (lane == 0) cluster_arrive(free_bar);
+                }
+                if (j < p.n && m0 + c < p.m) store_column<DT>(p, m0 + c, j, v);
+            }
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (*gave_up != 0 && tid == 0) {
+        if (p.status != nullptr) atomicOr(p.status, UQ_STATUS_TIMEOUT);
+        // copies of both CTAs that are still on their way must land before their memory is another's
+        const int n = *issued;
+        for (int i = n > ST ? n - ST : 0; rank == 0 && i < n; ++i) {
+            int again = 0;
+            barrier_wait(full + 8 * (i % ST), (i / ST) & 1, &again);
+        }
+    }
+    __syncwarp();
+    tensor_fence_before();
+    cluster_sync();                                        // the pair's other CTA is done with this one's memory
+    if (warp == 1) {
+        tensor_fence_after();
+        tmem_free<2>(tmem, 512);
     }
 }
 
@@ -200,6 +393,30 @@ bool codes_map(CUtensorMap *map, const uq_mx &q, int rows)
     return encode != nullptr &&
            encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, q.codes, size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Two scale tiles (1024 bytes) of `strips` strips of 128 rows.
+bool scales_map(CUtensorMap *map, const uq_mx &q, int strips)
+{
+    const EncodeTiled encode = encode_tiled();
+    const cuuint64_t size[2] = {(cuuint64_t)mx_ktiles(q.cols) * 128, (cuuint64_t)mx_ktiles(q.rows)}, stride[1] = {size[0] * 4};
+    const cuuint32_t box[2] = {256, (cuuint32_t)strips}, step[2] = {1, 1};
+    return encode != nullptr &&
+           encode(map, CU_TENSOR_MAP_DATA_TYPE_INT32, 2, q.scales, size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NT, int DT> cudaError_t launch_pairs(const uq_mx &a, const uq_mx &b, const ProductArgs &p, cudaStream_t st)
+{
+    using S = PairShape<NT>;
+    auto kernel = product_pair_kernel<NT, DT>;
+    CUtensorMap map_a, map_b, map_sa, map_sb;
+    if (!codes_map(&map_a, a, NT / 2) || !codes_map(&map_b, b, kRows) || !scales_map(&map_sa, a, (NT + 127) / 128) || !scales_map(&map_sb, b, 1))
+        return cudaErrorInvalidValue;
+    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+    const int64_t tiles = (p.n + 255) / 256 * ((p.m + NT - 1) / NT);
+    launch_k_smem(kernel, dim3((unsigned)(min(tiles, (int64_t)74) * 2)), dim3(kPThreads), S::kSmem, st, map_a, map_b, map_sa, map_sb, p);
+    return cudaGetLastError();
 }
 
 template <int NT, int DT> cudaError_t launch_tiles(const uq_mx &a, const uq_mx &b, ProductArgs p, cudaStream_t st)
@@ -236,6 +453,7 @@ template <int DT> cudaError_t launch_product(const uq_mx &a, const uq_mx &b, con
     if (p.m <= 16) return launch_tiles<16, DT>(a, b, p, st);
     if (p.m <= 32) return launch_tiles<32, DT>(a, b, p, st);
     if (p.m <= 64) return launch_tiles<64, DT>(a, b, p, st);
+    if ((p.n + 255) / 256 * ((p.m + 255) / 256) >= 74) return launch_pairs<256, DT>(a, b, p, st);
     return launch_tiles<128, DT>(a, b, p, st);
 }
 

@@ -26,7 +26,7 @@ __device__ __forceinline__ void barrier_arrive(uint32_t bar)
 __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
@@ -70,6 +70,11 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// An arrival at a barrier of any CTA of the cluster.
+__device__ __forceinline__ void cluster_arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+}
 __device__ __forceinline__ float cluster_load(uint32_t addr)
 {
     float v;
@@ -91,17 +96,31 @@ __device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap *map, 
                  :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 
+// The same for a pair of CTAs: into this CTA's memory, with the barrier (an address in the cluster) in either.
+__device__ __forceinline__ void copy_tile_pair(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
 // ---- tensor memory ------------------------------------------------------------------------------
 
-// By one whole warp; `columns` a power of two from 32 to 512.  The address lands in shared memory.
-__device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t columns)
+// CTAS = 2: the two CTAs of a pair work as one.  Allocation and release are by one whole warp (of both CTAs); `columns` a power
+// of two from 32 to 512; the address lands in shared memory.
+template <int CTAS> __device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t columns)
 {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(dst), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if constexpr (CTAS == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(dst), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(dst), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
 }
-__device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns)
+template <int CTAS> __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns)
 {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(columns));
+    if constexpr (CTAS == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(columns));
+    else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(columns));
 }
 __device__ __forceinline__ void tensor_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tensor_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -117,16 +136,22 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16])
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-// 512 bytes of scales (32 rows of 16 bytes in shared memory) into four columns, the same in each group of 32 lanes.
-__device__ __forceinline__ void tmem_copy_scales(uint32_t tmem, uint64_t desc)
+// 512 bytes of scales (32 rows of 16 bytes in shared memory) into four columns, the same in each group of 32 lanes; CTAS = 2: in
+// either CTA from its own shared memory.
+template <int CTAS> __device__ __forceinline__ void tmem_copy_scales(uint32_t tmem, uint64_t desc)
 {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(tmem), "l"(desc) : "memory");
+    if constexpr (CTAS == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" :: "r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" :: "r"(tmem), "l"(desc) : "memory");
 }
 
-// The barrier gets an arrival when everything that this thread has issued to the tensor core is done.
-__device__ __forceinline__ void tensor_commit(uint32_t bar)
+// The barrier (CTAS = 2: that of both CTAs) gets an arrival when everything that this thread has issued to the tensor core is done.
+template <int CTAS> __device__ __forceinline__ void tensor_commit(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+    if constexpr (CTAS == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     :: "r"(bar), "h"((uint16_t)3) : "memory");
 }
 
 // Shared-memory operand descriptors (address in 16-byte units; bit 46: the sm_100 form).  Matrix rows of 128 bytes in the
@@ -149,11 +174,16 @@ __host__ __device__ constexpr uint32_t mxf4_instruction(int m, int n, int half)
 }
 
 // 64 columns of both operands; accumulates onto D if `onto`.
-__device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t scale_a, uint32_t scale_b,
-                                         bool onto)
+template <int CTAS> __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t scale_a,
+                                                             uint32_t scale_b, bool onto)
 {
+    if constexpr (CTAS == 1)
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
                  "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"((uint32_t)onto) : "memory");
+    else
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
                  :: "r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"((uint32_t)onto) : "memory");
 }
 

@@ -197,7 +197,8 @@ def random_mx(rows, cols, seed, lo=124, hi=130):
 
 PRODUCTS = [(1, 1, 1), (1, 128, 32), (2, 5, 33), (7, 130, 64), (16, 256, 128), (17, 100, 260), (33, 129, 500), (64, 64, 256),
             (65, 300, 1000), (128, 128, 512), (129, 257, 777), (200, 1000, 96), (256, 512, 384), (300, 3, 2048), (1, 4096, 4096),
-            (13, 640, 5010), (513, 260, 4000), (1030, 700, 640)]
+            (13, 640, 5010), (513, 260, 4000), (1030, 700, 640),
+            (2100, 2200, 700), (2305, 2049, 300), (300, 19001, 256), (19003, 257, 130), (2200, 4500, 64)]
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
