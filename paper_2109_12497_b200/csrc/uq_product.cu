@@ -54,6 +54,32 @@ template <int DT> __device__ __forceinline__ void store_column(const ProductArgs
         if (t < have) store1<DT>(p.out, (i + t) * p.ld + j, v[t]);
 }
 
+// The multiplies of one stage: four of 64 columns (fewer in the row's last stage), with the copies of their scales to tensor
+// memory in front.  One thread issues everything that the tensor core does, so its instructions count: descriptors are their
+// low words plus constants, and nothing is decided in a whole stage.  `codes`, `scales`: low descriptor words of b's rows (a's
+// are A_AT bytes behind) and of b's scales (a's are 1024 bytes behind); `columns`: where the scales go.
+template <int CTAS, int NT, int A_AT> __device__ __forceinline__ void multiply_stage(uint32_t sums, uint32_t codes, uint32_t scales,
+                                                                                     uint32_t columns, int steps, bool onto)
+{
+    constexpr int M = CTAS * kRows, W = (NT + 127) / 128, HALF = 4 + 4 * W;
+    const auto operand = [](uint32_t lo) { return (uint64_t)lo | operand_descriptor(0) & 0xFFFFFFFF00000000ull; };
+    const auto scale = [](uint32_t lo) { return (uint64_t)lo | scales_descriptor(0) & 0xFFFFFFFF00000000ull; };
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                          // a scale tile: 128 columns
+        if (h == 1 && steps <= 2) break;
+        const uint32_t sb = columns + h * HALF, sa = sb + 4;
+        tmem_copy_scales<CTAS>(sb, scale(scales + h * (512 >> 4)));
+#pragma unroll
+        for (int w = 0; w < W; ++w) tmem_copy_scales<CTAS>(sa + 4 * w, scale(scales + ((1024 + w * 1024 + h * 512) >> 4)));
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            if (q == 1 && steps == 2 * h + 1) break;
+            const uint32_t at = codes + (2 * h + q) * (32 >> 4);
+            mma_mxf4<CTAS>(sums, operand(at), operand(at + (A_AT >> 4)), mxf4_instruction(M, NT, q), sb, sa, onto || h > 0 || q > 0);
+        }
+    }
+}
+
 template <int NT> struct ProductShape {
     static constexpr int kStageBytes = kRows * 128 + NT * 128 + 2048;
     static constexpr int kStages = NT == 128 ? 3 : 6;
@@ -101,40 +127,29 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
     const uint32_t tmem = *(volatile uint32_t *)tmem_slot;
 
     if (warp == 0 && lane == 0) {
-        for (int i = s0; i < s1; ++i) {
-            const int s = (i - s0) % ST, round = (i - s0) / ST;
-            if (round > 0 && !barrier_wait(empty + 8 * s, (round - 1) & 1, gave_up)) break;
+        const uint8_t *scales_b = p.scales_b + (n0 >> 7) * p.ktiles * 512, *scales_a = p.scales_a + (m0 >> 7) * p.ktiles * 512;
+        for (int i = s0, s = 0, parity = 1; i < s1; ++i) {
+            if (i - s0 >= ST && !barrier_wait(empty + 8 * s, parity, gave_up)) break;
             const uint32_t at = data + s * S::kStageBytes, bar = full + 8 * s;
             const uint32_t scale_bytes = p.ktiles - 2 * (int64_t)i >= 2 ? 1024 : 512;
             barrier_expect(bar, kRows * 128 + NT * 128 + 2 * scale_bytes);
             copy_tile(at, &map_b, i * 128, (int)n0, bar);
             copy_tile(at + kRows * 128, &map_a, i * 128, (int)m0, bar);
-            copy_bulk(at + kRows * 128 + NT * 128, p.scales_b + ((n0 >> 7) * p.ktiles + 2 * (int64_t)i) * 512, scale_bytes, bar);
-            copy_bulk(at + kRows * 128 + NT * 128 + 1024, p.scales_a + ((m0 >> 7) * p.ktiles + 2 * (int64_t)i) * 512, scale_bytes, bar);
+            copy_bulk(at + kRows * 128 + NT * 128, scales_b + (int64_t)i * 1024, scale_bytes, bar);
+            copy_bulk(at + kRows * 128 + NT * 128 + 1024, scales_a + (int64_t)i * 1024, scale_bytes, bar);
             *issued = i - s0 + 1;
+            if (++s == ST) { s = 0; parity ^= 1; }
         }
     } else if (warp == 1 && lane == 0) {
-        for (int i = s0; i < s1; ++i) {
-            const int s = (i - s0) % ST, round = (i - s0) / ST;
-            if (!barrier_wait(full + 8 * s, round & 1, gave_up)) break;
+        const uint32_t codes = (uint32_t)operand_descriptor(data), scales = (uint32_t)scales_descriptor(data + kRows * 128 + NT * 128);
+        for (int i = s0, s = 0, parity = 0; i < s1; ++i) {
+            if (!barrier_wait(full + 8 * s, parity, gave_up)) break;
             tensor_fence_after();
-            const uint32_t at = data + s * S::kStageBytes, scales = at + kRows * 128 + NT * 128;
-            const uint32_t sb = tmem + NT + s * S::kScaleColumns, sa = sb + 8;
-            const uint64_t db = operand_descriptor(at), da = operand_descriptor(at + kRows * 128);
-            const int64_t left = p.k - (int64_t)i * kStageK;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {                  // a scale tile: 128 columns
-                if (left > 128 * h) {
-                    tmem_copy_scales<1>(sb + 4 * h, scales_descriptor(scales + 512 * h));
-                    tmem_copy_scales<1>(sa + 4 * h, scales_descriptor(scales + 1024 + 512 * h));
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        if (left > 128 * h + 64 * q)
-                            mma_mxf4<1>(tmem, db + (2 * h + q) * 2, da + (2 * h + q) * 2, mxf4_instruction(kRows, NT, q), sb + 4 * h, sa + 4 * h,
-                                     i > s0 || h > 0 || q > 0);
-                }
-            }
+            const int steps = (int)min((int64_t)4, (p.k - (int64_t)i * kStageK + 63) >> 6);
+            multiply_stage<1, NT, kRows * 128>(tmem, codes + s * (S::kStageBytes >> 4), scales + s * (S::kStageBytes >> 4),
+                                               tmem + NT + s * S::kScaleColumns, steps, i > s0);
             tensor_commit<1>(empty + 8 * s);
+            if (++s == ST) { s = 0; parity ^= 1; }
         }
         tensor_commit<1>(done);
         int again = 0;                                     // (a wait of its own: tensor memory is given back only when nothing writes it)
@@ -261,57 +276,45 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 
     if (warp == 0 && lane == 0) {
         const uint32_t leader_full = cluster_address(full, 0);
-        int use = 0;                                       // how many stages this CTA has filled
+        int use = 0, s = 0, parity = 1;                    // stages filled so far; the next one, and the parity of its release
         for (int64_t t = pair; t < tiles && *gave_up == 0; t += pairs) {
             int64_t tm, tn;
             tile_place(t, tiles_m, tiles_n, &tm, &tn);
-            const int row_b = (int)(tn * 256 + rank * 128), row_a = (int)(tm * NT + rank * (NT / 2));
-            for (int i = 0; i < stages; ++i, ++use) {
-                const int s = use % ST, round = use / ST;
-                if (round > 0 && !barrier_wait(empty + 8 * s, (round - 1) & 1, gave_up)) break;
+            const int row_b = (int)(tn * 256 + rank * 128), row_a = (int)(tm * NT + rank * (NT / 2)), strip_a = (int)(tm * NT >> 7);
+            for (int i = 0; i < stages; ++i) {
+                if (use >= ST && !barrier_wait(empty + 8 * s, parity, gave_up)) break;
                 const uint32_t at = data + s * S::kStageBytes, bar = leader_full + 8 * s;
                 if (rank == 0) barrier_expect(full + 8 * s, 2 * S::kStageBytes);
                 copy_tile_pair(at, &map_b, i * 128, row_b, bar);
                 copy_tile_pair(at + kRows * 128, &map_a, i * 128, row_a, bar);
                 copy_tile_pair(at + kRows * 128 + NT / 2 * 128, &map_sb, i * 256, row_b >> 7, bar);
-                copy_tile_pair(at + kRows * 128 + NT / 2 * 128 + 1024, &map_sa, i * 256, (int)(tm * NT >> 7), bar);
-                *issued = use + 1;
+                copy_tile_pair(at + kRows * 128 + NT / 2 * 128 + 1024, &map_sa, i * 256, strip_a, bar);
+                *issued = ++use;
+                if (++s == ST) { s = 0; parity ^= 1; }
             }
         }
     } else if (warp == 1 && lane == 0 && rank == 0) {
-        int use = 0, turn = 0;
-        for (int64_t t = pair; t < tiles; t += pairs, ++turn) {
+        const uint32_t codes = (uint32_t)operand_descriptor(data), scales = (uint32_t)scales_descriptor(data + kRows * 128 + NT / 2 * 128);
+        const int last_steps = (int)((p.k - (int64_t)(stages - 1) * kStageK + 63) >> 6);
+        int s = 0, parity = 0, slot = 0, turn = 0;
+        int old = -S::kScaleSlots, old_parity = 0;         // the stage whose scales are overwritten (below 0: none yet)
+        bool going = true;
+        for (int64_t t = pair; going && t < tiles; t += pairs, ++turn) {
             if (turn > 0 && !barrier_wait(sums_free, (turn - 1) & 1, gave_up)) break;
             tensor_fence_after();
             const uint32_t sums = tmem + (turn & 1) * S::kSecond;
-            for (int i = 0; i < stages; ++i, ++use) {
-                const int s = use % ST;
-                const int before = use - S::kScaleSlots;   // the stage whose scales are overwritten
-                if (before >= 0 && !barrier_wait(empty + 8 * (before % ST), (before / ST) & 1, gave_up)) break;
-                if (!barrier_wait(full + 8 * s, (use / ST) & 1, gave_up)) break;
+            for (int i = 0; i < stages; ++i) {
+                going = (old < 0 || barrier_wait(empty + 8 * old, old_parity, gave_up)) && barrier_wait(full + 8 * s, parity, gave_up);
+                if (!going) break;
                 tensor_fence_after();
-                const uint32_t at = data + s * S::kStageBytes, scales = at + kRows * 128 + NT / 2 * 128;
-                const uint32_t slot = tmem + S::kScales + (use % S::kScaleSlots) * S::kSlotColumns;
-                const uint64_t db = operand_descriptor(at), da = operand_descriptor(at + kRows * 128);
-                const int64_t left = p.k - (int64_t)i * kStageK;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (left > 128 * h) {
-                        const uint32_t sb = slot + h * (S::kSlotColumns / 2), sa = sb + 4;
-                        tmem_copy_scales<2>(sb, scales_descriptor(scales + 512 * h));
-#pragma unroll
-                        for (int w = 0; w < (NT + 127) / 128; ++w) tmem_copy_scales<2>(sa + 4 * w, scales_descriptor(scales + 1024 * (1 + w) + 512 * h));
-#pragma unroll
-                        for (int q = 0; q < 2; ++q)
-                            if (left > 128 * h + 64 * q)
-                                mma_mxf4<2>(sums, db + (2 * h + q) * 2, da + (2 * h + q) * 2, mxf4_instruction(256, NT, q), sb, sa,
-                                            i > 0 || h > 0 || q > 0);
-                    }
-                }
+                multiply_stage<2, NT, kRows * 128>(sums, codes + s * (S::kStageBytes >> 4), scales + s * (S::kStageBytes >> 4),
+                                                   tmem + S::kScales + slot * S::kSlotColumns, i + 1 < stages ? 4 : last_steps, i > 0);
                 tensor_commit<2>(empty + 8 * s);
+                if (++s == ST) { s = 0; parity ^= 1; }
+                if (++slot == S::kScaleSlots) slot = 0;
+                if (++old == ST) { old = 0; old_parity ^= 1; }
             }
-            if (*gave_up != 0) break;
-            tensor_commit<2>(sums_ready);
+            if (going) tensor_commit<2>(sums_ready);
         }
         if (*gave_up != 0) {                               // tensor memory is given back only when nothing writes it
             int again = 0;

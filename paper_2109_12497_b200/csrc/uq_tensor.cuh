@@ -30,23 +30,20 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity)
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-__device__ __forceinline__ uint64_t nanoseconds()
-{
-    uint64_t t;
-    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
-}
 
-// Waits until the barrier's phase of that parity is complete, for two seconds at most; false, and *gave_up set for the CTA's other
-// waits to see, if it is not by then.
-constexpr uint64_t kWaitLimit = 2000000000ull;
+// Waits until the barrier's phase of that parity is complete, for about two seconds at most; false, and *gave_up set for the
+// CTA's other waits to see, if it is not by then.  (No timer is read while a wait is short.)
+constexpr long long kWaitCycles = 4000000000ll;
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int *gave_up)
 {
-    if (barrier_try(bar, parity)) return true;
-    const uint64_t start = nanoseconds();
+    long long start = 0;
     for (uint32_t i = 1;; ++i) {
         if (barrier_try(bar, parity)) return true;
-        if ((i & 63u) == 0 && (*gave_up != 0 || nanoseconds() - start > kWaitLimit)) break;
+        if ((i & 255u) == 0) {
+            const long long now = clock64();
+            if (start == 0) start = now;
+            if (*gave_up != 0 || now - start > kWaitCycles) break;
+        }
     }
     *gave_up = 1;
     return false;
