@@ -66,14 +66,14 @@ template <int CTAS, int NT, int A_AT> __device__ __forceinline__ void multiply_s
     const auto scale = [](uint32_t lo) { return (uint64_t)lo | scales_descriptor(0) & 0xFFFFFFFF00000000ull; };
 #pragma unroll
     for (int h = 0; h < 2; ++h) {                          // a scale tile: 128 columns
-        if (h == 1 && steps <= 2) break;
+        if (h == 1 && steps <= 2) continue;
         const uint32_t sb = columns + h * HALF, sa = sb + 4;
         tmem_copy_scales<CTAS>(sb, scale(scales + h * (512 >> 4)));
 #pragma unroll
         for (int w = 0; w < W; ++w) tmem_copy_scales<CTAS>(sa + 4 * w, scale(scales + ((1024 + w * 1024 + h * 512) >> 4)));
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            if (q == 1 && steps == 2 * h + 1) break;
+            if (q == 1 && steps == 2 * h + 1) continue;
             const uint32_t at = codes + (2 * h + q) * (32 >> 4);
             mma_mxf4<CTAS>(sums, operand(at), operand(at + (A_AT >> 4)), mxf4_instruction(M, NT, q), sb, sa, onto || h > 0 || q > 0);
         }
@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
     volatile int *gave_up = (volatile int *)(tmem_slot + 1);
     volatile int *issued = gave_up + 1;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     const uint32_t rank = p.split > 1 ? cluster_rank() : 0;
     const int64_t tiles_n = (p.n + kRows - 1) / kRows;
     const int64_t tile = blockIdx.x / p.split, n0 = tile % tiles_n * kRows, m0 = tile / tiles_n * NT;
@@ -126,39 +126,46 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
     tensor_fence_after();
     const uint32_t tmem = *(volatile uint32_t *)tmem_slot;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         const uint8_t *scales_b = p.scales_b + (n0 >> 7) * p.ktiles * 512, *scales_a = p.scales_a + (m0 >> 7) * p.ktiles * 512;
         for (int i = s0, s = 0, parity = 1; i < s1; ++i) {
-            if (i - s0 >= ST && !barrier_wait(empty + 8 * s, parity, gave_up)) break;
+            if (i - s0 >= ST && !barrier_wait_warp(empty + 8 * s, parity, gave_up)) break;
             const uint32_t at = data + s * S::kStageBytes, bar = full + 8 * s;
             const uint32_t scale_bytes = p.ktiles - 2 * (int64_t)i >= 2 ? 1024 : 512;
-            barrier_expect(bar, kRows * 128 + NT * 128 + 2 * scale_bytes);
-            copy_tile(at, &map_b, i * 128, (int)n0, bar);
-            copy_tile(at + kRows * 128, &map_a, i * 128, (int)m0, bar);
-            copy_bulk(at + kRows * 128 + NT * 128, scales_b + (int64_t)i * 1024, scale_bytes, bar);
-            copy_bulk(at + kRows * 128 + NT * 128 + 1024, scales_a + (int64_t)i * 1024, scale_bytes, bar);
-            *issued = i - s0 + 1;
+            if (elect_lane()) {
+                barrier_expect(bar, kRows * 128 + NT * 128 + 2 * scale_bytes);
+                copy_tile(at, &map_b, i * 128, (int)n0, bar);
+                copy_tile(at + kRows * 128, &map_a, i * 128, (int)m0, bar);
+                copy_bulk(at + kRows * 128 + NT * 128, scales_b + (int64_t)i * 1024, scale_bytes, bar);
+                copy_bulk(at + kRows * 128 + NT * 128 + 1024, scales_a + (int64_t)i * 1024, scale_bytes, bar);
+                *issued = i - s0 + 1;
+            }
+            __syncwarp();
             if (++s == ST) { s = 0; parity ^= 1; }
         }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         const uint32_t codes = (uint32_t)operand_descriptor(data), scales = (uint32_t)scales_descriptor(data + kRows * 128 + NT * 128);
         for (int i = s0, s = 0, parity = 0; i < s1; ++i) {
-            if (!barrier_wait(full + 8 * s, parity, gave_up)) break;
+            if (!barrier_wait_warp(full + 8 * s, parity, gave_up)) break;
             tensor_fence_after();
             const int steps = (int)min((int64_t)4, (p.k - (int64_t)i * kStageK + 63) >> 6);
-            multiply_stage<1, NT, kRows * 128>(tmem, codes + s * (S::kStageBytes >> 4), scales + s * (S::kStageBytes >> 4),
-                                               tmem + NT + s * S::kScaleColumns, steps, i > s0);
-            tensor_commit<1>(empty + 8 * s);
+            if (elect_lane()) {
+                multiply_stage<1, NT, kRows * 128>(tmem, codes + s * (S::kStageBytes >> 4), scales + s * (S::kStageBytes >> 4),
+                                                   tmem + NT + s * S::kScaleColumns, steps, i > s0);
+                tensor_commit<1>(empty + 8 * s);
+            }
+            __syncwarp();
             if (++s == ST) { s = 0; parity ^= 1; }
         }
-        tensor_commit<1>(done);
+        if (elect_lane()) tensor_commit<1>(done);
+        __syncwarp();
         int again = 0;                                     // (a wait of its own: tensor memory is given back only when nothing writes it)
-        if (!barrier_wait(done, 0, &again)) *gave_up = 1;
+        if (!barrier_wait_warp(done, 0, &again)) *gave_up = 1;
     }
     __syncwarp();
 
     if (warp >= 2) {
-        barrier_wait(done, 0, gave_up);
+        barrier_wait_warp(done, 0, gave_up);
         tensor_fence_after();
         const int quarter = warp & 3;
         const int64_t j = n0 + quarter * 32 + lane;
@@ -251,7 +258,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     volatile int *gave_up = (volatile int *)(tmem_slot + 1);
     volatile int *issued = gave_up + 1;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), lane = tid & 31;
     const uint32_t rank = cluster_rank();
     const int64_t tiles_n = (p.n + 255) / 256, tiles_m = (p.m + NT - 1) / NT, tiles = tiles_m * tiles_n;
     const int64_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -274,52 +281,63 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     tensor_fence_after();
     const uint32_t tmem = *(volatile uint32_t *)tmem_slot;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
         const uint32_t leader_full = cluster_address(full, 0);
         int use = 0, s = 0, parity = 1;                    // stages filled so far; the next one, and the parity of its release
-        for (int64_t t = pair; t < tiles && *gave_up == 0; t += pairs) {
+        bool going = true;
+        for (int64_t t = pair; going && t < tiles; t += pairs) {
             int64_t tm, tn;
             tile_place(t, tiles_m, tiles_n, &tm, &tn);
             const int row_b = (int)(tn * 256 + rank * 128), row_a = (int)(tm * NT + rank * (NT / 2)), strip_a = (int)(tm * NT >> 7);
             for (int i = 0; i < stages; ++i) {
-                if (use >= ST && !barrier_wait(empty + 8 * s, parity, gave_up)) break;
+                going = use < ST || barrier_wait_warp(empty + 8 * s, parity, gave_up);
+                if (!going) break;
                 const uint32_t at = data + s * S::kStageBytes, bar = leader_full + 8 * s;
-                if (rank == 0) barrier_expect(full + 8 * s, 2 * S::kStageBytes);
-                copy_tile_pair(at, &map_b, i * 128, row_b, bar);
-                copy_tile_pair(at + kRows * 128, &map_a, i * 128, row_a, bar);
-                copy_tile_pair(at + kRows * 128 + NT / 2 * 128, &map_sb, i * 256, row_b >> 7, bar);
-                copy_tile_pair(at + kRows * 128 + NT / 2 * 128 + 1024, &map_sa, i * 256, strip_a, bar);
-                *issued = ++use;
+                ++use;
+                if (elect_lane()) {
+                    if (rank == 0) barrier_expect(full + 8 * s, 2 * S::kStageBytes);
+                    copy_tile_pair(at, &map_b, i * 128, row_b, bar);
+                    copy_tile_pair(at + kRows * 128, &map_a, i * 128, row_a, bar);
+                    copy_tile_pair(at + kRows * 128 + NT / 2 * 128, &map_sb, i * 256, row_b >> 7, bar);
+                    copy_tile_pair(at + kRows * 128 + NT / 2 * 128 + 1024, &map_sa, i * 256, strip_a, bar);
+                    *issued = use;
+                }
+                __syncwarp();
                 if (++s == ST) { s = 0; parity ^= 1; }
             }
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         const uint32_t codes = (uint32_t)operand_descriptor(data), scales = (uint32_t)scales_descriptor(data + kRows * 128 + NT / 2 * 128);
         const int last_steps = (int)((p.k - (int64_t)(stages - 1) * kStageK + 63) >> 6);
         int s = 0, parity = 0, slot = 0, turn = 0;
         int old = -S::kScaleSlots, old_parity = 0;         // the stage whose scales are overwritten (below 0: none yet)
         bool going = true;
         for (int64_t t = pair; going && t < tiles; t += pairs, ++turn) {
-            if (turn > 0 && !barrier_wait(sums_free, (turn - 1) & 1, gave_up)) break;
+            if (turn > 0 && !barrier_wait_warp(sums_free, (turn - 1) & 1, gave_up)) break;
             tensor_fence_after();
             const uint32_t sums = tmem + (turn & 1) * S::kSecond;
             for (int i = 0; i < stages; ++i) {
-                going = (old < 0 || barrier_wait(empty + 8 * old, old_parity, gave_up)) && barrier_wait(full + 8 * s, parity, gave_up);
+                going = (old < 0 || barrier_wait_warp(empty + 8 * old, old_parity, gave_up)) && barrier_wait_warp(full + 8 * s, parity, gave_up);
                 if (!going) break;
                 tensor_fence_after();
-                multiply_stage<2, NT, kRows * 128>(sums, codes + s * (S::kStageBytes >> 4), scales + s * (S::kStageBytes >> 4),
-                                                   tmem + S::kScales + slot * S::kSlotColumns, i + 1 < stages ? 4 : last_steps, i > 0);
-                tensor_commit<2>(empty + 8 * s);
+                if (elect_lane()) {
+                    multiply_stage<2, NT, kRows * 128>(sums, codes + s * (S::kStageBytes >> 4), scales + s * (S::kStageBytes >> 4),
+                                                       tmem + S::kScales + slot * S::kSlotColumns, i + 1 < stages ? 4 : last_steps, i > 0);
+                    tensor_commit<2>(empty + 8 * s);
+                }
+                __syncwarp();
                 if (++s == ST) { s = 0; parity ^= 1; }
                 if (++slot == S::kScaleSlots) slot = 0;
                 if (++old == ST) { old = 0; old_parity ^= 1; }
             }
-            if (going) tensor_commit<2>(sums_ready);
+            if (going && elect_lane()) tensor_commit<2>(sums_ready);
+            __syncwarp();
         }
         if (*gave_up != 0) {                               // tensor memory is given back only when nothing writes it
             int again = 0;
-            tensor_commit<2>(drained);
-            barrier_wait(drained, 0, &again);
+            if (elect_lane()) tensor_commit<2>(drained);
+            __syncwarp();
+            barrier_wait_warp(drained, 0, &again);
         }
     } else if (warp >= 2) {
         const int quarter = warp & 3;
@@ -328,7 +346,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         for (int64_t t = pair; t < tiles; t += pairs, ++turn) {
             int64_t tm, tn;
             tile_place(t, tiles_m, tiles_n, &tm, &tn);
-            if (!barrier_wait(sums_ready, turn & 1, gave_up)) break;
+            if (!barrier_wait_warp(sums_ready, turn & 1, gave_up)) break;
             tensor_fence_after();
             const int64_t j = tn * 256 + rank * 128 + quarter * 32 + lane, m0 = tm * NT;
             const uint32_t sums = tmem + (turn & 1) * S::kSecond + ((uint32_t)(quarter * 32) << 16);

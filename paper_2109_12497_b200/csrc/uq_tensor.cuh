@@ -49,6 +49,31 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
     return false;
 }
 
+// The same by a whole warp, its lanes together.  (What a warp does together the compiler keeps in uniform registers, which is where
+// the copies and multiplies take their operands from: issued from a branch that one lane takes, they need a dozen moves each.)
+__device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity, volatile int *gave_up)
+{
+    long long start = 0;
+    for (uint32_t i = 1;; ++i) {
+        if (__all_sync(0xFFFFFFFFu, barrier_try(bar, parity))) return true;
+        if ((i & 255u) == 0) {
+            const long long now = clock64();
+            if (start == 0) start = now;
+            if (__any_sync(0xFFFFFFFFu, *gave_up != 0 || now - start > kWaitCycles)) break;
+        }
+    }
+    *gave_up = 1;
+    return false;
+}
+
+// True in one lane of a converged warp.
+__device__ __forceinline__ bool elect_lane()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+
 // ---- clusters -----------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t cluster_rank()
