@@ -24,6 +24,7 @@ struct ProductArgs {
 constexpr int kRows = 128;                                 // of b per tile
 constexpr int kStageK = 256;                               // columns per stage: 128 bytes of a row
 constexpr int kPThreads = 192;                             // warp 0 copies, warp 1 multiplies, warps 2 to 5 store
+constexpr int kPairThreads = 320;                          // ... warps 2 to 9
 
 template <int DT> __device__ __forceinline__ float load1(const void *base, int64_t at)
 {
@@ -37,21 +38,29 @@ template <int DT> __device__ __forceinline__ void store_result(const ProductArgs
     store1<DT>(p.out, i * p.ld + j, v);
 }
 
-// 16 rows of out from row i on, in one column: what is added is loaded first, all of it (it may be out itself, so the compiler
-// cannot move a load in front of a store).
-template <int DT> __device__ __forceinline__ void store_column(const ProductArgs &p, int64_t i, int64_t j, float (&v)[16])
+// 16 rows of out from row i on, in one column; `have` of them exist.
+template <int DT> __device__ __forceinline__ void load_column(const void *base, int64_t ld, int64_t i, int64_t j, int have, float (&v)[16])
 {
-    const int have = (int)min((int64_t)16, p.m - i);
-    if (p.add != nullptr) {
-        float w[16];
+    const char *at = (const char *)base + (i * ld + j) * Elem<DT>::BYTES;
+    if (have >= 16) {
 #pragma unroll
-        for (int t = 0; t < 16; ++t) w[t] = t < have ? load1<DT>(p.add, (i + t) * p.add_ld + j) : 0.0f;
+        for (int t = 0; t < 16; ++t, at += ld * Elem<DT>::BYTES) v[t] = load1<DT>(at, 0);
+    } else {
 #pragma unroll
-        for (int t = 0; t < 16; ++t) v[t] += w[t];
+        for (int t = 0; t < 16; ++t, at += ld * Elem<DT>::BYTES) v[t] = t < have ? load1<DT>(at, 0) : 0.0f;
     }
+}
+template <int DT> __device__ __forceinline__ void store_column(void *base, int64_t ld, int64_t i, int64_t j, int have, const float (&v)[16])
+{
+    char *at = (char *)base + (i * ld + j) * Elem<DT>::BYTES;
+    if (have >= 16) {
 #pragma unroll
-    for (int t = 0; t < 16; ++t)
-        if (t < have) store1<DT>(p.out, (i + t) * p.ld + j, v[t]);
+        for (int t = 0; t < 16; ++t, at += ld * Elem<DT>::BYTES) store1<DT>(at, 0, v[t]);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 16; ++t, at += ld * Elem<DT>::BYTES)
+            if (t < have) store1<DT>(at, 0, v[t]);
+    }
 }
 
 // The multiplies of one stage: four of 64 columns (fewer in the row's last stage), with the copies of their scales to tensor
@@ -180,8 +189,15 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
                 float *sums = (float *)base;               // every stage has been read: [column][lane]
 #pragma unroll
                 for (int t = 0; t < 16; ++t) sums[(c + t) * kRows + quarter * 32 + lane] = v[t];
-            } else if (j < p.n) {
-                store_column<DT>(p, m0 + c, j, v);
+            } else if (j < p.n && m0 + c < p.m) {
+                const int have = (int)min((int64_t)16, p.m - m0 - c);
+                if (p.add != nullptr) {                    // all of it first: it may be out itself, so no load moves in front of a store
+                    float w[16];
+                    load_column<DT>(p.add, p.add_ld, m0 + c, j, have, w);
+#pragma unroll
+                    for (int t = 0; t < 16; ++t) v[t] += w[t];
+                }
+                store_column<DT>(p.out, p.ld, m0 + c, j, have, v);
             }
         }
         tensor_fence_before();
@@ -243,7 +259,7 @@ __device__ __forceinline__ void tile_place(int64_t t, int64_t tiles_m, int64_t t
 }
 
 template <int NT, int DT>
-__global__ void __launch_bounds__(kPThreads) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1)
 product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                     const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb, const ProductArgs p)
 {
@@ -267,7 +283,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     grid_dependency_trigger();
     if (tid == 0) {
         for (int s = 0; s < 2 * ST + 1; ++s) barrier_init(full + 8 * s, 1);
-        barrier_init(sums_free, 8);                        // four warps of either CTA
+        barrier_init(sums_free, 16);                       // eight warps of either CTA
         barrier_init(drained, 1);
         *gave_up = 0;
         *issued = 0;
@@ -340,31 +356,43 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             barrier_wait_warp(drained, 0, &again);
         }
     } else if (warp >= 2) {
-        const int quarter = warp & 3;
+        // Two warps for each quarter of the lanes, taking turns of 16 columns.  What is added to a piece is loaded a piece ahead,
+        // the first piece's before the sums are there.
+        const int quarter = warp & 3, part = (warp - 2) >> 2;
         const uint32_t free_bar = cluster_address(sums_free, 0);
         int turn = 0;
         for (int64_t t = pair; t < tiles; t += pairs, ++turn) {
             int64_t tm, tn;
             tile_place(t, tiles_m, tiles_n, &tm, &tn);
-            if (!barrier_wait_warp(sums_ready, turn & 1, gave_up)) break;
-            tensor_fence_after();
             const int64_t j = tn * 256 + rank * 128 + quarter * 32 + lane, m0 = tm * NT;
             const uint32_t sums = tmem + (turn & 1) * S::kSecond + ((uint32_t)(quarter * 32) << 16);
             // the first of two overlapping tiles shares its last columns, the second its first
             const int first = (turn & 1) || S::kShared == 0 ? 0 : NT - S::kShared;
+            const auto column = [&](int done) { return first + done < NT ? first + done : first + done - NT; };
+            const auto rows_there = [&](int c) { return j < p.n ? (int)max((int64_t)0, min((int64_t)16, p.m - m0 - c)) : 0; };
+            float w[16];
+            if (p.add != nullptr) load_column<DT>(p.add, p.add_ld, m0 + column(part * 16), j, rows_there(column(part * 16)), w);
+            if (!barrier_wait_warp(sums_ready, turn & 1, gave_up)) break;
+            tensor_fence_after();
 #pragma unroll 1
-            for (int done = 0; done < NT; done += 16) {
-                const int c = first + done < NT ? first + done : first + done - NT;
+            for (int done = part * 16; done < NT; done += 32) {
+                const int c = column(done), have = rows_there(c);
                 float v[16];
                 __syncwarp();
                 tmem_load16(sums + c, v);
                 tmem_load_wait();
-                if (done + 16 == (S::kShared == 0 ? NT : S::kShared)) {
+                if (done < (S::kShared == 0 ? NT : S::kShared) && done + 32 >= (S::kShared == 0 ? NT : S::kShared)) {
                     tensor_fence_before();
                     __syncwarp();
                     if (lane == 0) cluster_arrive(free_bar);
                 }
-                if (j < p.n && m0 + c < p.m) store_column<DT>(p, m0 + c, j, v);
+                if (p.add != nullptr) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) v[k] += w[k];
+                    const int next = column(done + 32 < NT ? done + 32 : done);
+                    if (done + 32 < NT) load_column<DT>(p.add, p.add_ld, m0 + next, j, rows_there(next), w);
+                }
+                if (have > 0) store_column<DT>(p.out, p.ld, m0 + c, j, have, v);
             }
         }
     }
@@ -436,7 +464,7 @@ template <int NT, int DT> cudaError_t launch_pairs(const uq_mx &a, const uq_mx &
         return cudaErrorInvalidValue;
     cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
     const int64_t tiles = (p.n + 255) / 256 * ((p.m + NT - 1) / NT);
-    launch_k_smem(kernel, dim3((unsigned)(min(tiles, (int64_t)74) * 2)), dim3(kPThreads), S::kSmem, st, map_a, map_b, map_sa, map_sb, p);
+    launch_k_smem(kernel, dim3((unsigned)(min(tiles, (int64_t)74) * 2)), dim3(kPairThreads), S::kSmem, st, map_a, map_b, map_sa, map_sb, p);
     return cudaGetLastError();
 }
 
