@@ -2,9 +2,10 @@
 // from one read, and the values that codes stand for.
 //
 // A CTA owns a tile of 128 x 128 values: that is one scale tile of either orientation (512 contiguous bytes), and 64
-// contiguous bytes of every row of codes.  Rows: 16 lanes hold a row's 128 values, eight each; four lanes are a block, whose
-// largest magnitude two shuffles find.  Columns: the tile (and the draws, made once per eight values of a row and used in both
-// orientations) is kept in shared memory and read back two columns per lane.
+// contiguous bytes of every row of codes.  In either orientation a lane holds eight neighbours of a block and four lanes are a
+// block, whose largest magnitude two shuffles find.  Columns are read back from the tile in shared memory, bf16 values and the
+// draws (made once per eight values of a row, used in both orientations) by transposing matrix loads.
+// Bound by the arithmetic where it draws: see quantize_eight.
 #include "uq_mx.cuh"
 
 namespace uq {
@@ -12,146 +13,216 @@ namespace {
 
 constexpr int kQThreads = 256;
 
-template <int DT> struct TileWord;                        // two neighbouring columns of a row in shared memory
-template <> struct TileWord<UQ_BF16> { using T = uint32_t; };
-template <> struct TileWord<UQ_F32> { using T = uint2; };
+// The tile in shared memory.  16-bit elements: rows of 256 bytes whose 16-byte granules are exchanged so that the eight rows that
+// one transposing load takes (two neighbours at a distance of eight rows each) lie on different banks.  Binary32: rows of 528
+// bytes and 32 more after eight rows, for the same reason (a warp reads eight columns of four rows, eight rows apart).
+__device__ __forceinline__ uint32_t granule_at(int row, int granule) { return row * 256 + ((granule ^ (((row >> 3) & 3) * 2 + (row & 1))) << 4); }
+__device__ __forceinline__ uint32_t word_at(int row, int col) { return (row * 132 + (row >> 3) * 8 + col) * 4; }
+constexpr int kHalfTile = 128 * 256, kWordTile = (128 * 132 + 16 * 8) * 4;
+template <int DT> constexpr int kTileBytes = DT == UQ_BF16 ? kHalfTile : kWordTile;
 
-__device__ __forceinline__ float lo_of(uint32_t w) { return bf16lo(w); }
-__device__ __forceinline__ float hi_of(uint32_t w) { return bf16hi(w); }
-__device__ __forceinline__ float lo_of(uint2 w) { return __uint_as_float(w.x); }
-__device__ __forceinline__ float hi_of(uint2 w) { return __uint_as_float(w.y); }
-
-// Word (two columns) `c2` of row `r` of a tile in shared memory; eight words between groups of 32 rows keep the lanes of a
-// column pass (8 column pairs x 4 blocks) on different banks.
-__device__ __forceinline__ int tile_at(int r, int c2) { return r * 64 + (r >> 5) * 8 + c2; }
-constexpr int kTileWords = 128 * 64 + 4 * 8;
-
-template <int DT, bool SR>
-__global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__restrict__ x, int64_t rows, int64_t cols, int64_t ld,
-                                                                  PhiloxKey key, uq_mx q, uq_mx qt, uint32_t *status)
+// Eight rows (8 q .. 8 q + 7 of the 32 from `row` on, for q = lane % 4) of column `granule` * 8 + lane / 4 of a 16-bit tile, in
+// pairs: matrix i holds rows 2 i and 2 i + 1 of each group of eight.
+__device__ __forceinline__ uint4 column_of_halves(uint32_t tile, int row, int granule, int lane)
 {
-    using Word = typename TileWord<DT>::T;
+    const int i = lane >> 3, k = lane & 7;                 // this lane names row k of matrix i
+    const uint32_t at = tile + granule_at(row + 8 * (k >> 1) + 2 * i + (k & 1), granule);
+    uint4 v;
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+// The draws of eight neighbours of a row: Philox4x32-10 with counter (col / 8, row, 0, kMxTag).  Its third word is 0 and only the
+// second changes from row to row, so a thread that stays in its columns makes what the first two rounds take from the first,
+// third and fourth word once (DrawColumn), and 17 of the 20 wide multiplies are left.
+struct DrawColumn { uint32_t c0, c1, c3; };
+__device__ __forceinline__ DrawColumn draw_column(const PhiloxKey &k, uint32_t block)
+{
+    const uint64_t p0 = (uint64_t)kPhiloxM0 * block;       // round 0: c0 = row ^ k0, c1 = 0, c2 = hi ^ tag ^ k1, c3 = lo
+    const uint64_t p1 = (uint64_t)kPhiloxM1 * ((uint32_t)(p0 >> 32) ^ kMxTag ^ k.k[1]);
+    return {(uint32_t)(p1 >> 32) ^ k.k[2], (uint32_t)p1, (uint32_t)p0 ^ k.k[3]};
+}
+__device__ __forceinline__ uint4 draw_row(const PhiloxKey &k, const DrawColumn &d, uint32_t row)
+{
+    const uint64_t p = (uint64_t)kPhiloxM0 * (row ^ k.k[0]);
+    uint32_t c0 = d.c0, c1 = d.c1, c2 = (uint32_t)(p >> 32) ^ d.c3, c3 = (uint32_t)p;
+#pragma unroll
+    for (int r = 2; r < 10; ++r) {
+        const uint64_t p0 = (uint64_t)kPhiloxM0 * c0, p1 = (uint64_t)kPhiloxM1 * c2;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k.k[2 * r];
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k.k[2 * r + 1];
+        c1 = (uint32_t)p1; c3 = (uint32_t)p0;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+
+// Eight neighbours of a row of the tile in shared memory, and back.
+template <int DT> __device__ __forceinline__ void keep_eight(unsigned char *tile, int r, int chunk, const Eight<DT> &x)
+{
+    if constexpr (DT == UQ_BF16) {
+        *(uint4 *)(tile + granule_at(r, chunk)) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+    } else {
+        *(uint4 *)(tile + word_at(r, chunk * 8)) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+        *(uint4 *)(tile + word_at(r, chunk * 8 + 4)) = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+    }
+}
+template <int DT> __device__ __forceinline__ void kept_eight(const unsigned char *tile, int r, int chunk, Eight<DT> &x)
+{
+    if constexpr (DT == UQ_BF16) {
+        const uint4 q = *(const uint4 *)(tile + granule_at(r, chunk));
+        x.w[0] = q.x; x.w[1] = q.y; x.w[2] = q.z; x.w[3] = q.w;
+    } else {
+        const uint4 q = *(const uint4 *)(tile + word_at(r, chunk * 8)), q2 = *(const uint4 *)(tile + word_at(r, chunk * 8 + 4));
+        x.w[0] = q.x; x.w[1] = q.y; x.w[2] = q.z; x.w[3] = q.w;
+        x.w[4] = q2.x; x.w[5] = q2.y; x.w[6] = q2.z; x.w[7] = q2.w;
+    }
+}
+
+// WIDE: rows start on 16 bytes and consist of whole groups of eight; otherwise the tile is fetched element by element, a warp's
+// lanes side by side.
+template <int DT, bool SR, bool WIDE>
+__global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__restrict__ x, int64_t rows, int64_t cols, int64_t ld,
+                                                                  const PhiloxKey key, const uq_mx q, const uq_mx qt, uint32_t *status)
+{
+    constexpr int E = Elem<DT>::BYTES, BATCH = DT == UQ_BF16 ? 8 : 4;
     extern __shared__ __align__(16) unsigned char smem[];
-    Word *tile = (Word *)smem;
-    uint32_t *draws = (uint32_t *)(smem + sizeof(Word) * kTileWords);
+    const bool along_rows = q.codes != nullptr, along_cols = qt.codes != nullptr;
+    unsigned char *scales_q = smem, *scales_t = smem + 512, *tile = smem + 1024, *draws = tile + kTileBytes<DT>;
     grid_dependency_prologue();
     const int64_t ktq = mx_ktiles(cols), ktt = mx_ktiles(rows);
-    const int64_t r0 = blockIdx.x / ktq * kMxTile, c0 = blockIdx.x % ktq * kMxTile;
-    const int tid = threadIdx.x, lane = tid & 31;
-    const bool wide = ((uintptr_t)x & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0;
-    const bool along_rows = q.codes != nullptr, along_cols = qt.codes != nullptr;
+    const int64_t tr = blockIdx.x / ktq, tc = blockIdx.x % ktq, r0 = tr * kMxTile, c0 = tc * kMxTile;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rows_here = (int)min((int64_t)kMxTile, rows - r0), cols_here = (int)min((int64_t)kMxTile, cols - c0);
     bool bad = false;
 
-    const int chunk = tid & 15;                           // eight columns
-    const int64_t c = c0 + chunk * 8;
-    const int have = (int)min((int64_t)8, max((int64_t)0, cols - c));
-#pragma unroll 2
-    for (int r = tid >> 4; r < kMxTile; r += kQThreads / 16) {
-        const int64_t row = r0 + r;
-        const bool in = row < rows;
-        float v[8];
-        load8<DT>(x, row * ld + c, in ? have : 0, wide, v);
-        uint4 h = make_uint4(0, 0, 0, 0);
-        if constexpr (SR) h = philox4x32_10(key, (uint32_t)(c >> 3), (uint32_t)row, 0u, kMxTag);
-        if (along_cols) {
+    const int chunk = tid & 15, first = tid >> 4;          // eight columns, of every 16th row
+    if constexpr (!WIDE) {
+        for (int r = warp; r < kMxTile; r += kQThreads / 32) {
+            const char *row = (const char *)x + ((r0 + r) * ld + c0) * E;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                Word w;
-                if constexpr (DT == UQ_BF16) w = (__float_as_uint(v[2 * t]) >> 16) | (__float_as_uint(v[2 * t + 1]) & 0xFFFF0000u);
-                else w = make_uint2(__float_as_uint(v[2 * t]), __float_as_uint(v[2 * t + 1]));
-                tile[tile_at(r, chunk * 4 + t)] = w;
-            }
-            if constexpr (SR) {
-                uint32_t *d = draws + tile_at(r, chunk * 4);
-                d[0] = h.x; d[1] = h.y; d[2] = h.z; d[3] = h.w;
+            for (int c = lane; c < kMxTile; c += 32) {
+                const bool in = r < rows_here && c < cols_here;
+                if constexpr (DT == UQ_BF16)
+                    *(unsigned short *)(tile + granule_at(r, c >> 3) + (c & 7) * 2) = in ? __ldg((const unsigned short *)row + c) : (unsigned short)0;
+                else
+                    *(float *)(tile + word_at(r, c)) = in ? __ldg((const float *)row + c) : 0.0f;
             }
         }
-        if (along_rows) {
-            uint32_t m = max_abs_bits(v);
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-            m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-            const uint32_t byte = mx_scale_byte(m);
-            uint32_t codes = 0;
-            if (byte != 255u) {
-                const float inv = mx_inverse(byte);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) v[t] *= inv;
-                if constexpr (SR) codes = e2m1x8_stochastic(v, h);
-                else codes = e2m1x8_nearest(v);
-            } else {
-                bad = true;
-            }
-            if (in && c < mx_blocks(cols) * 32) *(uint32_t *)(q.codes + row * q.code_stride + (c >> 1)) = codes;
-            if ((lane & 3) == 0) q.scales[mx_scale_at(row, c >> 5, ktq)] = (uint8_t)(in ? byte : 0u);
-        }
-    }
-    if (along_cols) {
         __syncthreads();
-        const int block = (tid >> 3) & 3, pair = (tid >> 5) * 8 + (tid & 7);
-        uint32_t m0 = 0, m1 = 0;
-#pragma unroll 8
-        for (int t = 0; t < 32; ++t) {
-            const Word w = tile[tile_at(block * 32 + t, pair)];
-            m0 = max(m0, abs_bits(lo_of(w)));
-            m1 = max(m1, abs_bits(hi_of(w)));
-        }
-        const uint32_t b0 = mx_scale_byte(m0), b1 = mx_scale_byte(m1);
-        const float inv0 = b0 == 255u ? 0.0f : mx_inverse(b0), inv1 = b1 == 255u ? 0.0f : mx_inverse(b1);
-        bad = bad || b0 == 255u || b1 == 255u;
-        uint32_t out0[4], out1[4];
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            float v0[8], v1[8];
-            uint32_t h[8];
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                const int at = tile_at(block * 32 + g * 8 + t, pair);
-                const Word w = tile[at];
-                v0[t] = lo_of(w) * inv0;
-                v1[t] = hi_of(w) * inv1;
-                if constexpr (SR) h[t] = draws[at];
-            }
-            if constexpr (SR) {
-                uint4 e, o;
-                e.x = __byte_perm(h[0], h[1], 0x5410); o.x = __byte_perm(h[0], h[1], 0x7632);
-                e.y = __byte_perm(h[2], h[3], 0x5410); o.y = __byte_perm(h[2], h[3], 0x7632);
-                e.z = __byte_perm(h[4], h[5], 0x5410); o.z = __byte_perm(h[4], h[5], 0x7632);
-                e.w = __byte_perm(h[6], h[7], 0x5410); o.w = __byte_perm(h[6], h[7], 0x7632);
-                out0[g] = e2m1x8_stochastic(v0, e);
-                out1[g] = e2m1x8_stochastic(v1, o);
-            } else {
-                out0[g] = e2m1x8_nearest(v0);
-                out1[g] = e2m1x8_nearest(v1);
-            }
-            if (b0 == 255u) out0[g] = 0;
-            if (b1 == 255u) out1[g] = 0;
-        }
-        const int64_t col = c0 + pair * 2, blk = (r0 >> 5) + block;
-        const bool inb = blk < mx_blocks(rows);
-        if (col < cols && inb) *(uint4 *)(qt.codes + col * qt.code_stride + blk * 16) = make_uint4(out0[0], out0[1], out0[2], out0[3]);
-        if (col + 1 < cols && inb) *(uint4 *)(qt.codes + (col + 1) * qt.code_stride + blk * 16) = make_uint4(out1[0], out1[1], out1[2], out1[3]);
-        qt.scales[mx_scale_at(col, blk, ktt)] = (uint8_t)(inb ? b0 : 0u);
-        qt.scales[mx_scale_at(col + 1, blk, ktt)] = (uint8_t)(inb ? b1 : 0u);
     }
+    const DrawColumn mine = draw_column(key, (uint32_t)((c0 >> 3) + chunk));
+#pragma unroll 1
+    for (int batch = 0; batch < 8; batch += BATCH) {
+        Eight<DT> v[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int r = first + (batch + k) * 16;
+            if constexpr (WIDE) {
+                uint4 a = make_uint4(0, 0, 0, 0), b = a;
+                if (r < rows_here && chunk * 8 < cols_here) {
+                    const char *at = (const char *)x + ((r0 + r) * ld + c0 + chunk * 8) * E;
+                    a = ld_stream(at);
+                    if constexpr (DT == UQ_F32) b = ld_stream(at + 16);
+                }
+                v[k].w[0] = a.x; v[k].w[1] = a.y; v[k].w[2] = a.z; v[k].w[3] = a.w;
+                if constexpr (DT == UQ_F32) { v[k].w[4] = b.x; v[k].w[5] = b.y; v[k].w[6] = b.z; v[k].w[7] = b.w; }
+            } else {
+                kept_eight<DT>(tile, r, chunk, v[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int r = first + (batch + k) * 16;
+            uint4 h = make_uint4(0, 0, 0, 0);
+            if constexpr (SR) h = draw_row(key, mine, (uint32_t)(r0 + r));
+            if (along_cols) {
+                if constexpr (WIDE) keep_eight<DT>(tile, r, chunk, v[k]);
+                if constexpr (SR) *(uint4 *)(draws + granule_at(r, chunk)) = h;
+            }
+            if (along_rows) {
+                uint32_t byte;
+                const uint32_t codes = quantize_eight<DT, SR>(v[k], h, byte);
+                bad = bad || byte == 255u;
+                if (r < rows_here && chunk * 8 < ((cols_here + 31) & ~31))
+                    *(uint32_t *)(q.codes + (r0 + r) * q.code_stride + ((c0 + chunk * 8) >> 1)) = codes;
+                if ((lane & 3) == 0) scales_q[(r & 31) * 16 + (r >> 5) * 4 + (chunk >> 2)] = (uint8_t)byte;
+            }
+        }
+    }
+    __syncthreads();
+    if (along_cols) {
+        // a warp: 16 columns in two groups of eight, the four blocks of each
+        const int group = lane >> 2, part = lane & 3;
+#pragma unroll 1
+        for (int g = warp * 2; g < warp * 2 + 2; ++g) {
+            const int col = g * 8 + group;
+            unsigned char *out = qt.codes + (c0 + col) * qt.code_stride + r0 / 2 + part * 4;
+#pragma unroll
+            for (int blk = 0; blk < 4; ++blk) {
+                Eight<DT> v;
+                uint4 h = make_uint4(0, 0, 0, 0);
+                if constexpr (DT == UQ_BF16) {
+                    const uint4 w = column_of_halves(smem_address(tile), blk * 32, g, lane);
+                    v.w[0] = w.x; v.w[1] = w.y; v.w[2] = w.z; v.w[3] = w.w;
+                } else {
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) v.w[t] = *(const uint32_t *)(tile + word_at(blk * 32 + part * 8 + t, col));
+                }
+                if constexpr (SR) h = column_of_halves(smem_address(draws), blk * 32, g, lane);
+                uint32_t byte;
+                const uint32_t codes = quantize_eight<DT, SR>(v, h, byte);
+                bad = bad || byte == 255u;
+                if (col < cols_here && blk * 32 < rows_here) *(uint32_t *)(out + blk * 16) = codes;
+                if (part == 0) scales_t[(col & 31) * 16 + (col >> 5) * 4 + blk] = (uint8_t)byte;
+            }
+        }
+        __syncthreads();
+    }
+    if (along_rows && warp == 0) *(uint4 *)(q.scales + (tr * ktq + tc) * 512 + lane * 16) = *(const uint4 *)(scales_q + lane * 16);
+    if (along_cols && warp == 1) *(uint4 *)(qt.scales + (tc * ktt + tr) * 512 + lane * 16) = *(const uint4 *)(scales_t + lane * 16);
     if (status != nullptr && bad) atomicOr(status, UQ_STATUS_NONFINITE);
 }
 
-// Eight values per thread.
+// ---- values -------------------------------------------------------------------------------------
+
+// bf16 patterns of four magnitude codes, as their high and low bytes: a byte permute looks four codes up at once.
+__device__ __forceinline__ uint32_t code_high_bytes(uint32_t codes) { return __byte_perm(0x3F3F3F00u, 0x40404040u, codes & 0x7777u); }
+__device__ __forceinline__ uint32_t code_low_bytes(uint32_t codes) { return __byte_perm(0xC0800000u, 0xC0804000u, codes & 0x7777u); }
+
+// The values of eight codes, without their scale, as bf16 pairs.
+__device__ __forceinline__ void code_values(uint32_t codes, uint32_t (&w)[4])
+{
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const uint32_t c = codes >> (16 * half), hi = code_high_bytes(c), lo = code_low_bytes(c);
+        // signs: bits 3, 7, 11, 15 of c
+        const uint32_t s0 = ((c << 12) & 0x8000u) | ((c << 24) & 0x80000000u), s1 = ((c << 4) & 0x8000u) | ((c << 16) & 0x80000000u);
+        w[2 * half] = __byte_perm(lo, hi, 0x5140) | s0;
+        w[2 * half + 1] = __byte_perm(lo, hi, 0x7362) | s1;
+    }
+}
+
+// A warp takes pieces of 256 columns of a row, eight values a lane.
 template <int DT>
-__global__ void __launch_bounds__(kQThreads) dequantize_kernel(uq_mx q, void *__restrict__ out, int64_t ld)
+__global__ void __launch_bounds__(kQThreads) dequantize_kernel(const uq_mx q, void *__restrict__ out, int64_t ld)
 {
     grid_dependency_prologue();
-    const int64_t chunks = (q.cols + 7) >> 3, kt = mx_ktiles(q.cols);
+    const int64_t pieces = (q.cols + 255) >> 8, kt = mx_ktiles(q.cols), n = q.rows * pieces, step = (int64_t)gridDim.x * (kQThreads / 32);
     const bool wide = ((uintptr_t)out & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0;
-    const int64_t n = q.rows * chunks, step = (int64_t)gridDim.x * kQThreads;
-    for (int64_t i = (int64_t)blockIdx.x * kQThreads + threadIdx.x; i < n; i += step) {
-        const int64_t row = i / chunks, c = (i - row * chunks) * 8;
+    const int lane = threadIdx.x & 31;
+    for (int64_t i = (int64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5); i < n; i += step) {
+        const int64_t row = i / pieces, c = (i - row * pieces) * 256 + lane * 8;
+        const int have = (int)max((int64_t)0, min((int64_t)8, q.cols - c));
+        if (have == 0) continue;
         const uint32_t codes = __ldg((const uint32_t *)(q.codes + row * q.code_stride + (c >> 1)));
         const float scale = mx_scale_value(__ldg(q.scales + mx_scale_at(row, c >> 5, kt)));
+        uint32_t w[4];
         float v[8];
+        code_values(codes, w);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) v[t] = mx_code_value(codes >> (4 * t)) * scale;
-        store8<DT>(out, row * ld + c, (int)min((int64_t)8, q.cols - c), wide, v);
+        for (int t = 0; t < 4; ++t) mul_pair(bf16lo(w[t]), bf16hi(w[t]), scale, scale, v[2 * t], v[2 * t + 1]);
+        store8<DT>(out, row * ld + c, have, wide, v);
     }
 }
 
@@ -159,8 +230,10 @@ template <int DT, bool SR>
 void launch_tile(const void *x, int64_t rows, int64_t cols, int64_t ld, const PhiloxKey &key, const uq_mx &q, const uq_mx &qt,
                  uint32_t *status, cudaStream_t st)
 {
-    const size_t smem = qt.codes == nullptr ? 0 : (size_t)kTileWords * ((DT == UQ_BF16 ? 4 : 8) + (SR ? 4 : 0));
-    auto kernel = quantize_tile_kernel<DT, SR>;
+    const bool wide = ((uintptr_t)x & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0 && (cols & 7) == 0;
+    const bool tile = !wide || qt.codes != nullptr;
+    const size_t smem = 1024 + (tile ? kTileBytes<DT> + (SR && qt.codes != nullptr ? kHalfTile : 0) : 0);
+    auto kernel = wide ? quantize_tile_kernel<DT, SR, true> : quantize_tile_kernel<DT, SR, false>;
     if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     launch_k_smem(kernel, dim3((unsigned)(mx_ktiles(cols) * mx_ktiles(rows))), dim3(kQThreads), smem, st, x, rows, cols, ld, key, q, qt,
                   status);
@@ -184,8 +257,8 @@ cudaError_t launch_mx_quantize(const void *x, int64_t rows, int64_t cols, int64_
 
 cudaError_t launch_mx_dequantize(const uq_mx &q, void *out, int64_t ld, int dtype, cudaStream_t st)
 {
-    const int64_t n = q.rows * ((q.cols + 7) >> 3);
-    const unsigned grid = (unsigned)min((n + kQThreads - 1) / kQThreads, (int64_t)148 * 64);
+    const int64_t warps = q.rows * ((q.cols + 255) >> 8);
+    const unsigned grid = (unsigned)min((warps * 32 + kQThreads - 1) / kQThreads, (int64_t)148 * 64);
     if (dtype == UQ_BF16) launch_k(dequantize_kernel<UQ_BF16>, dim3(grid), dim3(kQThreads), st, q, out, ld);
     else launch_k(dequantize_kernel<UQ_F32>, dim3(grid), dim3(kQThreads), st, q, out, ld);
     return cudaGetLastError();

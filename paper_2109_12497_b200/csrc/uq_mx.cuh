@@ -40,22 +40,6 @@ __device__ __forceinline__ float mx_scale_value(uint32_t byte)
     return byte == 255u ? __uint_as_float(0x7FFFFFFFu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
 }
 
-// The value of a 4-bit code: magnitude bits in the top of a binary32 subnormal or small normal, times 2^126 (exact).
-__device__ __forceinline__ float mx_code_value(uint32_t code)
-{
-    return __uint_as_float(((code & 8u) << 28) | ((code & 7u) << 22)) * __uint_as_float(253u << 23);
-}
-
-// Magnitude code of a in [0, 6], rounded up iff h < rint(p * 2^16).  With u = 0.5, 1 or 2 the grid's step at a, adding
-// 2^23 * (u / 2^16) leaves rint(a / u * 2^16) in the sum's low bits (one rounding, ties to even); steps before this binade
-// are added as 2 * 2^16 per binade, and 2^16 - 1 - h carries into the code iff h is below the fraction.
-__device__ __forceinline__ uint32_t e2m1_stochastic(float a, uint32_t h)
-{
-    const uint32_t e = max(__float_as_uint(a) & 0x7F800000u, 0x3F800000u), magic = e + (6u << 23);
-    const uint32_t t = __float_as_uint(__fadd_rn(a, __uint_as_float(magic))) - magic + ((e - 0x3F800000u) >> 6);
-    return (t + 65535u - h) >> 16;
-}
-
 // Eight values rounded to the nearest code, ties to the even one (the conversion's own rule), element 0 in the low bits.
 __device__ __forceinline__ uint32_t e2m1x8_nearest(const float (&v)[8])
 {
@@ -68,18 +52,115 @@ __device__ __forceinline__ uint32_t e2m1x8_nearest(const float (&v)[8])
     return r;
 }
 
-// Eight values with their 16-bit draws (word t holds those of elements 2 t and 2 t + 1, low half first).
-__device__ __forceinline__ uint32_t e2m1x8_stochastic(const float (&v)[8], const uint4 &draws)
+// c + a * b of two values at once.
+__device__ __forceinline__ void fma_pair(float a0, float a1, float b, float c, float &r0, float &r1)
 {
-    const uint32_t w[4] = {draws.x, draws.y, draws.z, draws.w};
-    uint32_t r = 0;
+    uint64_t x, y, z, r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a0), "f"(a1));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(y) : "f"(b));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(z) : "f"(c));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(x), "l"(y), "l"(z));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r0), "=f"(r1) : "l"(r));
+}
+
+// Byte B of each of four words, in their order.
+template <int B> __device__ __forceinline__ uint32_t same_byte(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3)
+{
+    constexpr uint32_t sel = B | (4 + B) << 4;
+    return __byte_perm(__byte_perm(w0, w1, sel), __byte_perm(w2, w3, sel), 0x5410);
+}
+
+// Magnitude codes (bits 16 to 18 of `code`; what lies above and below is not defined) of two values of magnitude a * inv in
+// [0, 6], rounded up iff h < rint(p * 2^16).  The codes' values 0, 0.5 .. 2, 3, 4, 6 are the places where a concave function of
+// three pieces takes whole numbers: with a' = a * inv it is half of min(2 a', a' + 2, a' / 2 + 4) (slopes 2, 1, 1/2 up to 2, 4, 6).
+// Each piece plus 64 is one fused multiply-add with a single rounding, to 2^-17, ties to even: the minimum's low bits are
+// code * 2^16 + rint(p * 2^16).  2^16 - 1 - h carries into the code iff h is below the fraction.
+__device__ __forceinline__ void e2m1_stochastic_pair(float a0, float a1, float inv, uint32_t h0, uint32_t h1, uint32_t &code0, uint32_t &code1)
+{
+    float s0, s1, t0, t1, u0, u1;
+    fma_pair(a0, a1, inv, 64.0f, s0, s1);
+    fma_pair(a0, a1, 0.5f * inv, 65.0f, t0, t1);
+    fma_pair(a0, a1, 0.25f * inv, 66.0f, u0, u1);
+    asm("min.f32 %0, %0, %1, %2;" : "+f"(s0) : "f"(t0), "f"(u0));
+    asm("min.f32 %0, %0, %1, %2;" : "+f"(s1) : "f"(t1), "f"(u1));
+    code0 = __float_as_uint(s0) + 65535u - h0;             // 64 has no bits below bit 23
+    code1 = __float_as_uint(s1) + 65535u - h1;
+}
+
+// Eight neighbouring values as they lie in memory.
+template <int DT> struct Eight;
+template <> struct Eight<UQ_BF16> {
+    uint32_t w[4];
+    __device__ __forceinline__ uint32_t max_abs_bits() const              // of the binary32 values
+    {
+        uint32_t m = w[0] & 0x7FFF7FFFu;
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-        const uint32_t h = (t & 1) ? w[t >> 1] >> 16 : w[t >> 1] & 0xFFFFu;
-        const uint32_t code = e2m1_stochastic(fabsf(v[t]), h) | ((__float_as_uint(v[t]) >> 28) & 8u);
-        r |= code << (4 * t);
+        for (int t = 1; t < 4; ++t) m = __vmaxu2(m, w[t] & 0x7FFF7FFFu);
+        return max(m << 16, m & 0xFFFF0000u);
     }
-    return r;
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) { v[2 * t] = bf16lo(w[t]); v[2 * t + 1] = bf16hi(w[t]); }
+    }
+    __device__ __forceinline__ void magnitudes(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) { v[2 * t] = bf16lo(w[t] & 0x7FFF7FFFu); v[2 * t + 1] = bf16hi(w[t] & 0x7FFF7FFFu); }
+    }
+    // signs in bit 7 of the bytes: of elements 0, 2, 4, 6 and of 1, 3, 5, 7
+    __device__ __forceinline__ uint32_t even_signs() const { return same_byte<1>(w[0], w[1], w[2], w[3]); }
+    __device__ __forceinline__ uint32_t odd_signs() const { return same_byte<3>(w[0], w[1], w[2], w[3]); }
+};
+template <> struct Eight<UQ_F32> {
+    uint32_t w[8];
+    __device__ __forceinline__ uint32_t max_abs_bits() const
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) m = max(m, w[t] & 0x7FFFFFFFu);
+        return m;
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = __uint_as_float(w[t]);
+    }
+    __device__ __forceinline__ void magnitudes(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = __uint_as_float(w[t] & 0x7FFFFFFFu);
+    }
+    __device__ __forceinline__ uint32_t even_signs() const { return same_byte<3>(w[0], w[2], w[4], w[6]); }
+    __device__ __forceinline__ uint32_t odd_signs() const { return same_byte<3>(w[1], w[3], w[5], w[7]); }
+};
+
+// A lane's eight values of a block that it shares with three neighbouring lanes: its codes, and the block's scale byte.  draws:
+// word t holds those of elements 2 t and 2 t + 1, low half first.  The warp is converged.
+template <int DT, bool SR> __device__ __forceinline__ uint32_t quantize_eight(const Eight<DT> &x, const uint4 &draws, uint32_t &byte)
+{
+    uint32_t m = x.max_abs_bits();
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+    m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+    byte = mx_scale_byte(m);
+    const float inv = mx_inverse(byte);                    // (of a block that is not finite: anything)
+    uint32_t codes;
+    float v[8];
+    if constexpr (SR) {
+        const uint32_t h[4] = {draws.x, draws.y, draws.z, draws.w};
+        uint32_t c[8];
+        x.magnitudes(v);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) e2m1_stochastic_pair(v[2 * t], v[2 * t + 1], inv, h[t] & 0xFFFFu, h[t] >> 16, c[2 * t], c[2 * t + 1]);
+        const uint32_t even = same_byte<2>(c[0], c[2], c[4], c[6]), odd = same_byte<2>(c[1], c[3], c[5], c[7]);
+        codes = (even & 0x07070707u) | ((x.even_signs() >> 4) & 0x08080808u) | ((odd << 4) & 0x70707070u) | (x.odd_signs() & 0x80808080u);
+    } else {
+        x.values(v);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) mul_pair(v[2 * t], v[2 * t + 1], inv, inv, v[2 * t], v[2 * t + 1]);
+        codes = e2m1x8_nearest(v);
+    }
+    return byte == 255u ? 0u : codes;
 }
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
