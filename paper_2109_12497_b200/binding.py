@@ -538,48 +538,76 @@ class MxMatrix:
         self._ref = C.byref(self.c)
         self._index = codes.get_device()
 
-    def ref(self):
-        """The C struct, for a launch on the current device."""
-        if self._index < 0:
-            raise ValueError("uq: tensors must live on a CUDA device")
-        if self._index != _current_device():
-            require_current_device(self._index, torch.cuda.current_device(), "a microscaled matrix")
+    def ref(self, device: int):
+        """The C struct, beside tensors of that device."""
+        if self._index != device:
+            _refuse_device(self._index, device, "a microscaled matrix")
         return self._ref
 
 
+# The host's share of a call is as long as a small call's kernel, so these ask torch for as little as the checks need: a call's
+# tensors are compared with the first one's device, and that with the current one, once.
+
+def _refuse_device(index: int, device: int, what: str) -> None:
+    if index < 0 or device < 0:
+        raise ValueError("uq: tensors must live on a CUDA device")
+    raise ValueError(f"uq: {what} lives on CUDA device {index}, the call's first tensor on {device}")
+
+
+def _stream_of(device: int) -> int:
+    """The current stream of a call's device, which has to be the current one."""
+    if device < 0:
+        raise ValueError("uq: tensors must live on a CUDA device")
+    if device != _current_device():
+        require_current_device(device, _current_device())
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+_DTYPES = {torch.float32: UQ_F32, torch.bfloat16: UQ_BF16}
+
+
 def _dtype(t: torch.Tensor, what: str) -> int:
-    if t.dtype is torch.bfloat16:
-        return UQ_BF16
-    if t.dtype is torch.float32:
-        return UQ_F32
-    raise ValueError(f"uq: {what} must be float32 or bfloat16")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"uq: {what} must be float32 or bfloat16")
+    return code
 
 
-def _matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, what: str) -> int:
-    """Checks a matrix whose rows are contiguous and returns the elements between its rows."""
+def _matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, device: int, what: str):
+    """Checks a matrix whose rows are contiguous: its address, and the elements between its rows."""
     if t.dtype is not dtype or t.dim() != 2:
         raise ValueError(f"uq: {what} must be a 2-D {dtype} tensor")
-    r, c = t.shape
-    if r != rows or c != cols:
-        raise ValueError(f"uq: {what} must be [{rows}, {cols}], not [{r}, {c}]")
+    if t.shape != (rows, cols):
+        raise ValueError(f"uq: {what} must be [{rows}, {cols}], not {list(t.shape)}")
     step, inner = t.stride()
     if (inner != 1 and cols > 1) or (step < cols and rows > 1):
         raise ValueError(f"uq: the rows of {what} must be contiguous and must not overlap")
-    return step if rows > 1 else max(step, cols)
+    index = t.get_device()
+    if index != device:
+        _refuse_device(index, device, what)
+    return t.data_ptr(), step if step > cols else cols
 
 
-def _vector(t: Optional[torch.Tensor], n: int, what: str, dtype: torch.dtype = torch.float32) -> Optional[int]:
+def _vector(t: Optional[torch.Tensor], n: int, device: int, what: str, dtype: torch.dtype = torch.float32) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != n or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"uq: {what} must be a contiguous 1-D {dtype} tensor with {n} elements")
-    return _ptr(t)
+    index = t.get_device()
+    if index != device:
+        _refuse_device(index, device, what)
+    return t.data_ptr()
 
 
-def _status(t: Optional[torch.Tensor]) -> Optional[int]:
-    if t is not None and (t.dtype is not torch.int32 or t.numel() < 1):
+def _status(t: Optional[torch.Tensor], device: int) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() < 1:
         raise ValueError("uq: status must be an int32 tensor")
-    return _ptr(t)
+    index = t.get_device()
+    if index != device:
+        _refuse_device(index, device, "status")
+    return t.data_ptr()
 
 
 def _shape(t: torch.Tensor, what: str):
@@ -592,17 +620,19 @@ def uq_mx_quantize(x: torch.Tensor, seed: int, rng_bits: int, q: Optional[MxMatr
                    status: Optional[torch.Tensor] = None) -> None:
     """x [rows, cols] to microscaled 4-bit values: ``q`` with blocks along the rows, ``qt`` = the transposed matrix with
     blocks along x's columns, or both.  rng_bits 0: to the nearest value; 16: stochastically, unbiased."""
+    device = x.get_device()
     (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
-    ld = _matrix(x, rows, cols, x.dtype, "x")
+    px, ld = _matrix(x, rows, cols, x.dtype, device, "x")
     _check("uq_mx_quantize", lib().uq_mx_quantize(
-        _ptr(x), rows, cols, ld, dtype, seed & 0xFFFFFFFFFFFFFFFF, rng_bits, None if q is None else q.ref(),
-        None if qt is None else qt.ref(), _status(status), _stream()))
+        px, rows, cols, ld, dtype, seed & 0xFFFFFFFFFFFFFFFF, rng_bits, None if q is None else q.ref(device),
+        None if qt is None else qt.ref(device), _status(status, device), _stream_of(device)))
 
 
 def uq_mx_dequantize(q: MxMatrix, out: torch.Tensor) -> None:
     """The values that a microscaled matrix stands for (exact in either type)."""
-    dtype, ld = _dtype(out, "out"), _matrix(out, q.rows, q.cols, out.dtype, "out")
-    _check("uq_mx_dequantize", lib().uq_mx_dequantize(q.ref(), _ptr(out), ld, dtype, _stream()))
+    device = out.get_device()
+    dtype, (po, ld) = _dtype(out, "out"), _matrix(out, q.rows, q.cols, out.dtype, device, "out")
+    _check("uq_mx_dequantize", lib().uq_mx_dequantize(q.ref(device), po, ld, dtype, _stream_of(device)))
 
 
 def uq_mx_product(a: MxMatrix, b: MxMatrix, out: torch.Tensor, add: Optional[torch.Tensor] = None,
@@ -610,22 +640,25 @@ def uq_mx_product(a: MxMatrix, b: MxMatrix, out: torch.Tensor, add: Optional[tor
     """out [a.rows, b.rows] = a b^T (+ add, which may be out itself), binary32 sums rounded once to out's type."""
     if a.cols != b.cols:
         raise ValueError(f"uq: the operands have {a.cols} and {b.cols} columns")
-    dtype, ld = _dtype(out, "out"), _matrix(out, a.rows, b.rows, out.dtype, "out")
-    add_ld = 0 if add is None else _matrix(add, a.rows, b.rows, out.dtype, "add")
-    _check("uq_mx_product", lib().uq_mx_product(a.ref(), b.ref(), _ptr(add), add_ld, _ptr(out), ld, dtype,
-                                                _status(status), _stream()))
+    device = out.get_device()
+    dtype, (po, ld) = _dtype(out, "out"), _matrix(out, a.rows, b.rows, out.dtype, device, "out")
+    pa, add_ld = (None, 0) if add is None else _matrix(add, a.rows, b.rows, out.dtype, device, "add")
+    _check("uq_mx_product", lib().uq_mx_product(a.ref(device), b.ref(device), pa, add_ld, po, ld, dtype, _status(status, device),
+                                                _stream_of(device)))
 
 
 def uq_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
                   y: Optional[torch.Tensor], mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None,
                   q: Optional[MxMatrix] = None, status: Optional[torch.Tensor] = None) -> None:
     """Layer norm over the rows of x; any of y, the statistics and the quantized y (q) may be left out."""
+    device = x.get_device()
     (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
-    ld = _matrix(x, rows, cols, x.dtype, "x")
-    y_ld = 0 if y is None else _matrix(y, rows, cols, x.dtype, "y")
+    px, ld = _matrix(x, rows, cols, x.dtype, device, "x")
+    py, y_ld = (None, 0) if y is None else _matrix(y, rows, cols, x.dtype, device, "y")
     _check("uq_layer_norm", lib().uq_layer_norm(
-        _ptr(x), rows, cols, ld, dtype, _vector(gamma, cols, "gamma"), _vector(beta, cols, "beta"), eps, _ptr(y), y_ld,
-        _vector(mean, rows, "mean"), _vector(rstd, rows, "rstd"), None if q is None else q.ref(), _status(status), _stream()))
+        px, rows, cols, ld, dtype, _vector(gamma, cols, device, "gamma"), _vector(beta, cols, device, "beta"), eps, py, y_ld,
+        _vector(mean, rows, device, "mean"), _vector(rstd, rows, device, "rstd"), None if q is None else q.ref(device),
+        _status(status, device), _stream_of(device)))
 
 
 def uq_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
@@ -637,16 +670,20 @@ def uq_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[to
                            dbeta: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
     """Gradients of uq_layer_norm; dgamma and dbeta (float32 or bfloat16, both the same) may be pieces of a worker's row
     of gradients.  ``workspace``: uq_layer_norm_workspace_bytes(rows, cols) bytes."""
-    rows, cols = _shape(x, "x")
-    x_ld = _matrix(x, rows, cols, x.dtype, "x")
-    dy_ld = _matrix(dy, rows, cols, x.dtype, "dy")
-    dx_ld = 0 if dx is None else _matrix(dx, rows, cols, x.dtype, "dx")
+    device = x.get_device()
+    (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
+    px, x_ld = _matrix(x, rows, cols, x.dtype, device, "x")
+    pdy, dy_ld = _matrix(dy, rows, cols, x.dtype, device, "dy")
+    pdx, dx_ld = (None, 0) if dx is None else _matrix(dx, rows, cols, x.dtype, device, "dx")
     grad = dgamma if dgamma is not None else dbeta
     grad_dtype = torch.float32 if grad is None else grad.dtype
     if not workspace.is_contiguous():
         raise ValueError("uq: the workspace must be contiguous")
+    index = workspace.get_device()
+    if index != device:
+        _refuse_device(index, device, "the workspace")
     _check("uq_layer_norm_backward", lib().uq_layer_norm_backward(
-        _ptr(dy), dy_ld, _ptr(x), x_ld, rows, cols, _dtype(x, "x"), _vector(gamma, cols, "gamma"), _vector(mean, rows, "mean"),
-        _vector(rstd, rows, "rstd"), _ptr(dx), dx_ld, _vector(dgamma, cols, "dgamma", grad_dtype),
-        _vector(dbeta, cols, "dbeta", grad_dtype), UQ_F32 if grad is None else _dtype(grad, "dgamma and dbeta"),
-        _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+        pdy, dy_ld, px, x_ld, rows, cols, dtype, _vector(gamma, cols, device, "gamma"), _vector(mean, rows, device, "mean"),
+        _vector(rstd, rows, device, "rstd"), pdx, dx_ld, _vector(dgamma, cols, device, "dgamma", grad_dtype),
+        _vector(dbeta, cols, device, "dbeta", grad_dtype), UQ_F32 if grad is None else _dtype(grad, "dgamma and dbeta"),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_of(device)))

@@ -63,8 +63,11 @@ template <int DT> __device__ __forceinline__ void keep_eight(unsigned char *tile
     if constexpr (DT == UQ_BF16) {
         *(uint4 *)(tile + granule_at(r, chunk)) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
     } else {
-        *(uint4 *)(tile + word_at(r, chunk * 8)) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
-        *(uint4 *)(tile + word_at(r, chunk * 8 + 4)) = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+        // four lanes their first half, the next four their second: eight lanes then cover all banks
+        const bool second = chunk & 4;
+        const uint4 a = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]), b = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+        *(uint4 *)(tile + word_at(r, chunk * 8 + (second ? 4 : 0))) = second ? b : a;
+        *(uint4 *)(tile + word_at(r, chunk * 8 + (second ? 0 : 4))) = second ? a : b;
     }
 }
 template <int DT> __device__ __forceinline__ void kept_eight(const unsigned char *tile, int r, int chunk, Eight<DT> &x)
@@ -203,26 +206,47 @@ __device__ __forceinline__ void code_values(uint32_t codes, uint32_t (&w)[4])
     }
 }
 
-// A warp takes pieces of 256 columns of a row, eight values a lane.
-template <int DT>
+// A warp takes pieces of 256 columns of a row: eight neighbours a lane, or, where rows of out do not start on 16 bytes, eight
+// values that are 32 apart, so that a store is contiguous.
+template <int DT, bool WIDE>
 __global__ void __launch_bounds__(kQThreads) dequantize_kernel(const uq_mx q, void *__restrict__ out, int64_t ld)
 {
     grid_dependency_prologue();
-    const int64_t pieces = (q.cols + 255) >> 8, kt = mx_ktiles(q.cols), n = q.rows * pieces, step = (int64_t)gridDim.x * (kQThreads / 32);
-    const bool wide = ((uintptr_t)out & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0;
+    const int64_t pieces = (q.cols + 255) >> 8, kt = mx_ktiles(q.cols), step = (int64_t)gridDim.x * (kQThreads / 32);
+    const int64_t row_step = step / pieces, piece_step = step - row_step * pieces;      // (one division, not one for every piece)
     const int lane = threadIdx.x & 31;
-    for (int64_t i = (int64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5); i < n; i += step) {
-        const int64_t row = i / pieces, c = (i - row * pieces) * 256 + lane * 8;
-        const int have = (int)max((int64_t)0, min((int64_t)8, q.cols - c));
-        if (have == 0) continue;
-        const uint32_t codes = __ldg((const uint32_t *)(q.codes + row * q.code_stride + (c >> 1)));
-        const float scale = mx_scale_value(__ldg(q.scales + mx_scale_at(row, c >> 5, kt)));
-        uint32_t w[4];
-        float v[8];
-        code_values(codes, w);
+    const int64_t start = (int64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5);
+    int64_t row = start / pieces, piece = start - row * pieces;
+    while (row < q.rows) {
+        if constexpr (WIDE) {
+            const int64_t c = piece * 256 + lane * 8;
+            if (c < q.cols) {
+                const uint32_t codes = __ldg((const uint32_t *)(q.codes + row * q.code_stride + (c >> 1)));
+                const float scale = mx_scale_value(__ldg(q.scales + mx_scale_at(row, c >> 5, kt)));
+                uint32_t w[4];
+                float v[8];
+                code_values(codes, w);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) mul_pair(bf16lo(w[t]), bf16hi(w[t]), scale, scale, v[2 * t], v[2 * t + 1]);
-        store8<DT>(out, row * ld + c, have, wide, v);
+                for (int t = 0; t < 4; ++t) mul_pair(bf16lo(w[t]), bf16hi(w[t]), scale, scale, v[2 * t], v[2 * t + 1]);
+                store8<DT>(out, row * ld + c, (int)min((int64_t)8, q.cols - c), true, v);
+            }
+        } else {
+            const unsigned char *codes = q.codes + row * q.code_stride + piece * 128 + (lane >> 1);
+            const uint8_t *scales = q.scales + mx_scale_at(row, piece * 8, kt);
+            const int64_t left = q.cols - piece * 256 - lane;
+            char *at = (char *)out + (row * ld + piece * 256 + lane) * Elem<DT>::BYTES;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                if (32 * t < left) {                       // (block t of the piece: in its first or second scale tile)
+                    const uint32_t code = (uint32_t)__ldg(codes + 16 * t) >> (4 * (lane & 1)) & 15u;
+                    const float v = mx_code_value(code) * mx_scale_value(__ldg(scales + (t >> 2) * 512 + (t & 3)));
+                    store1<DT>(at, 32 * t, v);
+                }
+            }
+        }
+        row += row_step;
+        piece += piece_step;
+        if (piece >= pieces) { piece -= pieces; ++row; }
     }
 }
 
@@ -259,8 +283,9 @@ cudaError_t launch_mx_dequantize(const uq_mx &q, void *out, int64_t ld, int dtyp
 {
     const int64_t warps = q.rows * ((q.cols + 255) >> 8);
     const unsigned grid = (unsigned)min((warps * 32 + kQThreads - 1) / kQThreads, (int64_t)148 * 64);
-    if (dtype == UQ_BF16) launch_k(dequantize_kernel<UQ_BF16>, dim3(grid), dim3(kQThreads), st, q, out, ld);
-    else launch_k(dequantize_kernel<UQ_F32>, dim3(grid), dim3(kQThreads), st, q, out, ld);
+    const bool wide = ((uintptr_t)out & 15) == 0 && (ld * (dtype == UQ_BF16 ? 2 : 4) & 15) == 0;
+    if (dtype == UQ_BF16) launch_k(wide ? dequantize_kernel<UQ_BF16, true> : dequantize_kernel<UQ_BF16, false>, dim3(grid), dim3(kQThreads), st, q, out, ld);
+    else launch_k(wide ? dequantize_kernel<UQ_F32, true> : dequantize_kernel<UQ_F32, false>, dim3(grid), dim3(kQThreads), st, q, out, ld);
     return cudaGetLastError();
 }
 

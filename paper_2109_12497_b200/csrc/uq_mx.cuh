@@ -163,6 +163,12 @@ template <int DT, bool SR> __device__ __forceinline__ uint32_t quantize_eight(co
     return byte == 255u ? 0u : codes;
 }
 
+// The value of a 4-bit code: magnitude bits in the top of a binary32 subnormal or small normal, times 2^126 (exact).
+__device__ __forceinline__ float mx_code_value(uint32_t code)
+{
+    return __uint_as_float(((code & 8u) << 28) | ((code & 7u) << 22)) * __uint_as_float(253u << 23);
+}
+
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
 __device__ __forceinline__ uint32_t max_abs_bits(const float (&v)[8])

@@ -28,9 +28,9 @@ def test_sizes(lib):
     assert lib.uq_layer_norm_workspace_bytes(-1, 5) == 0 and lib.uq_layer_norm_workspace_bytes(0, 5) == 0
     assert lib.uq_layer_norm_workspace_bytes(1, 5) >= 2 * 5 * 4
     last = 0
-    for rows in (1, 10, 100, 1000, 10 ** 6):                 # more rows never need less, and at most a few megabytes a 1000 columns
+    for rows in (1, 10, 100, 1000, 10 ** 6):                 # more rows never need less, and at most some megabytes for 1000 columns
         n = lib.uq_layer_norm_workspace_bytes(rows, 1000)
-        assert last <= n <= 8 << 20
+        assert last <= n <= 16 << 20
         last = n
 
 
