@@ -101,14 +101,16 @@ template <int DT, int MAP, int PE> __device__ __forceinline__ void load_piece(co
             v[t] = q.x; v[t + 1] = q.y; v[t + 2] = q.z; v[t + 3] = q.w;
         }
     } else {
+        const auto element = [&](int i) {
+            if constexpr (DT == UQ_BF16) return __uint_as_float((uint32_t)*(const unsigned short *)(row + i * 2) << 16);
+            else return *(const float *)(row + i * 4);
+        };
+        if (at + (PE - 1) * piece_step<MAP>() < cols) {    // (all but the last pieces: no questions asked)
 #pragma unroll
-        for (int t = 0; t < PE; ++t) {
-            const int i = at + t * piece_step<MAP>();
-            v[t] = 0.0f;
-            if (i < cols) {
-                if constexpr (DT == UQ_BF16) v[t] = __uint_as_float((uint32_t)*(const unsigned short *)(row + i * 2) << 16);
-                else v[t] = *(const float *)(row + i * 4);
-            }
+            for (int t = 0; t < PE; ++t) v[t] = element(at + t * piece_step<MAP>());
+        } else {
+#pragma unroll
+            for (int t = 0; t < PE; ++t) v[t] = at + t * piece_step<MAP>() < cols ? element(at + t * piece_step<MAP>()) : 0.0f;
         }
     }
 }
@@ -119,6 +121,9 @@ template <int DT, int MAP, int PE> __device__ __forceinline__ void store_piece(v
         *(float4 *)((float *)row + at) = make_float4(v[0], v[1], v[2], v[3]);
     } else if constexpr (is_wide(MAP)) {
         store8<DT>(row, at, 8, true, v);
+    } else if (at + (PE - 1) * piece_step<MAP>() < cols) {
+#pragma unroll
+        for (int t = 0; t < PE; ++t) store1<DT>(row, at + t * piece_step<MAP>(), v[t]);
     } else {
 #pragma unroll
         for (int t = 0; t < PE; ++t)

@@ -198,55 +198,102 @@ __device__ __forceinline__ void code_values(uint32_t codes, uint32_t (&w)[4])
 {
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-        const uint32_t c = codes >> (16 * half), hi = code_high_bytes(c), lo = code_low_bytes(c);
-        // signs: bits 3, 7, 11, 15 of c
-        const uint32_t s0 = ((c << 12) & 0x8000u) | ((c << 24) & 0x80000000u), s1 = ((c << 4) & 0x8000u) | ((c << 16) & 0x80000000u);
-        w[2 * half] = __byte_perm(lo, hi, 0x5140) | s0;
-        w[2 * half + 1] = __byte_perm(lo, hi, 0x7362) | s1;
+        const uint32_t c = half ? codes >> 16 : codes;
+        const uint32_t twice = __byte_perm(c, 0, 0x1100), low_nibbles = twice << 4;       // signs to bit 7 of four bytes
+        const uint32_t signs = (low_nibbles & 0x00FF00FFu) | (twice & 0xFF00FF00u);
+        const uint32_t hi = code_high_bytes(c) | (signs & 0x80808080u), lo = code_low_bytes(c);
+        w[2 * half] = __byte_perm(lo, hi, 0x5140);
+        w[2 * half + 1] = __byte_perm(lo, hi, 0x7362);
     }
 }
 
-// A warp takes pieces of 256 columns of a row: eight neighbours a lane, or, where rows of out do not start on 16 bytes, eight
-// values that are 32 apart, so that a store is contiguous.
+// 2^e as a bf16 pair; products with it are exact (subnormal results too).
+__device__ __forceinline__ uint32_t scale_pair(uint32_t byte)
+{
+    const uint32_t v = byte == 255u ? 0x7FFFu : byte == 0u ? 0x0040u : byte << 7;
+    return v | v << 16;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// A warp takes units of 256 columns of four rows: eight neighbours a lane (binary32: four, and four 128 columns on), or, where
+// rows of out do not start on 16 bytes, a row, eight values a lane that are 32 apart: a store is contiguous.
+constexpr int kDequantRows = 4;
 template <int DT, bool WIDE>
 __global__ void __launch_bounds__(kQThreads) dequantize_kernel(const uq_mx q, void *__restrict__ out, int64_t ld)
 {
     grid_dependency_prologue();
+    constexpr int R = WIDE ? kDequantRows : 1;
     const int64_t pieces = (q.cols + 255) >> 8, kt = mx_ktiles(q.cols), step = (int64_t)gridDim.x * (kQThreads / 32);
-    const int64_t row_step = step / pieces, piece_step = step - row_step * pieces;      // (one division, not one for every piece)
+    const int64_t row_step = step / pieces, piece_step = step - row_step * pieces;      // (one division, not one for every unit)
     const int lane = threadIdx.x & 31;
     const int64_t start = (int64_t)blockIdx.x * (kQThreads / 32) + (threadIdx.x >> 5);
-    int64_t row = start / pieces, piece = start - row * pieces;
-    while (row < q.rows) {
+    int64_t group = start / pieces, piece = start - group * pieces;
+    while (group * R < q.rows) {
+        const int64_t row = group * R;
+        const int there = (int)min((int64_t)R, q.rows - row);
         if constexpr (WIDE) {
-            const int64_t c = piece * 256 + lane * 8;
-            if (c < q.cols) {
-                const uint32_t codes = __ldg((const uint32_t *)(q.codes + row * q.code_stride + (c >> 1)));
-                const float scale = mx_scale_value(__ldg(q.scales + mx_scale_at(row, c >> 5, kt)));
-                uint32_t w[4];
-                float v[8];
-                code_values(codes, w);
+            constexpr int N = DT == UQ_BF16 ? 8 : 4;
 #pragma unroll
-                for (int t = 0; t < 4; ++t) mul_pair(bf16lo(w[t]), bf16hi(w[t]), scale, scale, v[2 * t], v[2 * t + 1]);
-                store8<DT>(out, row * ld + c, (int)min((int64_t)8, q.cols - c), true, v);
-            }
-        } else {
-            const unsigned char *codes = q.codes + row * q.code_stride + piece * 128 + (lane >> 1);
-            const uint8_t *scales = q.scales + mx_scale_at(row, piece * 8, kt);
-            const int64_t left = q.cols - piece * 256 - lane;
-            char *at = (char *)out + (row * ld + piece * 256 + lane) * Elem<DT>::BYTES;
+            for (int k = 0; k < 8 / N; ++k) {
+                const int64_t c = piece * 256 + k * 128 + lane * N;
+                if (c >= q.cols) break;
+                const unsigned char *codes = q.codes + row * q.code_stride + (c >> 1);
+                const uint8_t *scales = q.scales + mx_scale_at(row, c >> 5, kt);        // the rows' are 16 bytes apart
+                char *at = (char *)out + (row * ld + c) * Elem<DT>::BYTES;
+                const int have = (int)min((int64_t)N, q.cols - c);
+                uint32_t code[R], byte[R];
 #pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                if (32 * t < left) {                       // (block t of the piece: in its first or second scale tile)
-                    const uint32_t code = (uint32_t)__ldg(codes + 16 * t) >> (4 * (lane & 1)) & 15u;
-                    const float v = mx_code_value(code) * mx_scale_value(__ldg(scales + (t >> 2) * 512 + (t & 3)));
-                    store1<DT>(at, 32 * t, v);
+                for (int r = 0; r < R; ++r)
+                    if (r < there) {
+                        if constexpr (N == 8) code[r] = __ldg((const uint32_t *)(codes + r * q.code_stride));
+                        else code[r] = __ldg((const unsigned short *)(codes + r * q.code_stride));
+                        byte[r] = __ldg(scales + 16 * r);
+                    }
+#pragma unroll
+                for (int r = 0; r < R; ++r, at += ld * Elem<DT>::BYTES) {
+                    if (r >= there) break;
+                    uint32_t w[4];
+                    code_values(code[r], w);
+                    if (DT == UQ_BF16 && have == N) {
+                        const uint32_t scale = scale_pair(byte[r]);
+                        *(uint4 *)at = make_uint4(mul_bf16x2(w[0], scale), mul_bf16x2(w[1], scale), mul_bf16x2(w[2], scale), mul_bf16x2(w[3], scale));
+                    } else {
+                        const float scale = mx_scale_value(byte[r]);
+                        float v[8];
+#pragma unroll
+                        for (int t = 0; t < N / 2; ++t) mul_pair(bf16lo(w[t]), bf16hi(w[t]), scale, scale, v[2 * t], v[2 * t + 1]);
+                        if (DT == UQ_F32 && have == N) *(float4 *)at = make_float4(v[0], v[1], v[2], v[3]);
+                        else {
+#pragma unroll
+                            for (int t = 0; t < N; ++t)
+                                if (t < have) store1<DT>(at, t, v[t]);
+                        }
+                    }
                 }
             }
+        } else {
+            // lane l fetches codes 8 l .. 8 l + 7 of the piece and (of the first eight lanes) the scale of block l
+            const int64_t first = piece * 256, left = q.cols - first - lane;
+            uint32_t codes = 0, byte = 0;
+            if (first + lane * 8 < q.cols) codes = __ldg((const uint32_t *)(q.codes + row * q.code_stride + (first >> 1)) + lane);
+            if (lane < 8 && first + lane * 32 < q.cols) byte = __ldg(q.scales + mx_scale_at(row, piece * 8 + lane, kt));
+            const float mine = mx_scale_value(byte);
+            char *at = (char *)out + (row * ld + first + lane) * Elem<DT>::BYTES;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+                const uint32_t code = __shfl_sync(0xFFFFFFFFu, codes, 4 * t + (lane >> 3)) >> (4 * (lane & 7));
+                const float scale = __shfl_sync(0xFFFFFFFFu, mine, t);
+                if (32 * t < left) store1<DT>(at, 32 * t, mx_code_value(code) * scale);
+            }
         }
-        row += row_step;
+        group += row_step;
         piece += piece_step;
-        if (piece >= pieces) { piece -= pieces; ++row; }
+        if (piece >= pieces) { piece -= pieces; ++group; }
     }
 }
 
@@ -281,9 +328,9 @@ cudaError_t launch_mx_quantize(const void *x, int64_t rows, int64_t cols, int64_
 
 cudaError_t launch_mx_dequantize(const uq_mx &q, void *out, int64_t ld, int dtype, cudaStream_t st)
 {
-    const int64_t warps = q.rows * ((q.cols + 255) >> 8);
-    const unsigned grid = (unsigned)min((warps * 32 + kQThreads - 1) / kQThreads, (int64_t)148 * 64);
     const bool wide = ((uintptr_t)out & 15) == 0 && (ld * (dtype == UQ_BF16 ? 2 : 4) & 15) == 0;
+    const int64_t warps = (wide ? (q.rows + kDequantRows - 1) / kDequantRows : q.rows) * ((q.cols + 255) >> 8);
+    const unsigned grid = (unsigned)min((warps * 32 + kQThreads - 1) / kQThreads, (int64_t)148 * 64);
     if (dtype == UQ_BF16) launch_k(wide ? dequantize_kernel<UQ_BF16, true> : dequantize_kernel<UQ_BF16, false>, dim3(grid), dim3(kQThreads), st, q, out, ld);
     else launch_k(wide ? dequantize_kernel<UQ_F32, true> : dequantize_kernel<UQ_F32, false>, dim3(grid), dim3(kQThreads), st, q, out, ld);
     return cudaGetLastError();

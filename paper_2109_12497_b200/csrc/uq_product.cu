@@ -91,7 +91,7 @@ template <int CTAS, int NT, int A_AT> __device__ __forceinline__ void multiply_s
 
 template <int NT> struct ProductShape {
     static constexpr int kStageBytes = kRows * 128 + NT * 128 + 2048;
-    static constexpr int kStages = NT == 128 ? 3 : 6;
+    static constexpr int kStages = NT == 128 ? 3 : NT == 16 ? 5 : 4;      // two CTAs fit an SM
     static constexpr int kScaleColumns = 16;               // per stage: 2 x 4 of each operand
     static constexpr int kColumns = NT + kStages * kScaleColumns <= 128 ? 128 : 256;
     static constexpr int kSmem = kStages * kStageBytes + 1024 + 256;
@@ -219,12 +219,24 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
     }
     if (p.split > 1) {
         cluster_sync();
-        const int share = NT / p.split;
-        for (int e = tid; e < share * kRows; e += kPThreads) {
-            const int c = (int)rank * share + e / kRows, l = e % kRows;
-            float v = 0.0f;
-            for (int r = 0; r < p.split; ++r) v += cluster_load(cluster_address(data + (c * kRows + l) * 4, r));
-            if (m0 + c < p.m && n0 + l < p.n) store_result<DT>(p, m0 + c, n0 + l, v);
+        // Four neighbouring rows of b per thread, from all CTAs in their order; the loads of several columns in flight together.
+        const int c0 = NT * (int)rank / p.split, c1 = NT * ((int)rank + 1) / p.split;
+        for (int e = tid; e < (c1 - c0) * (kRows / 4); e += kPThreads) {
+            const int c = c0 + e / (kRows / 4), l = e % (kRows / 4) * 4;
+            if (m0 + c >= p.m) continue;
+            float4 w[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < p.split) w[r] = cluster_load4(cluster_address(data + (c * kRows + l) * 4, r));
+            float4 v = w[0];
+#pragma unroll
+            for (int r = 1; r < 8; ++r)
+                if (r < p.split) { v.x += w[r].x; v.y += w[r].y; v.z += w[r].z; v.w += w[r].w; }
+            const int64_t left = p.n - n0 - l;
+            if (left > 0) store_result<DT>(p, m0 + c, n0 + l, v.x);
+            if (left > 1) store_result<DT>(p, m0 + c, n0 + l + 1, v.y);
+            if (left > 2) store_result<DT>(p, m0 + c, n0 + l + 2, v.z);
+            if (left > 3) store_result<DT>(p, m0 + c, n0 + l + 3, v.w);
         }
         cluster_sync();                                    // the others may still be reading here
     }
@@ -468,6 +480,22 @@ template <int NT, int DT> cudaError_t launch_pairs(const uq_mx &a, const uq_mx &
     return cudaGetLastError();
 }
 
+// CTAs that share a tile's columns, from measured costs in microseconds: a stage takes 0.22 + 0.0018 NT of one CTA on an SM (two on
+// an SM share it), joining the sums of s CTAs 1.6 + 0.035 NT + 0.2 s.
+// 4 x 4096 x 4096: 5.3 alone, 4.5 by four; 64 x 8192 x 8192: 13.3 and 11.1;
+// 512 x 4096 x 4096, which has an SM for each tile as it is: 8.0 and, by two, 12.9.
+int best_split(int nt, int64_t tiles, int64_t stages)
+{
+    int best = 1;
+    double least = 1e30;
+    for (int s = 1; s <= 8 && s <= stages && (s == 1 || tiles * s <= 296); s *= 2) {
+        const double load = tiles * s > 148 ? (double)(tiles * s) / 148.0 : 1.0;
+        const double t = load * (double)((stages + s - 1) / s) * (0.22 + 0.0018 * nt) + (s > 1 ? 1.6 + 0.035 * nt + 0.2 * s : 0.0);
+        if (t < least) { least = t; best = s; }
+    }
+    return best;
+}
+
 template <int NT, int DT> cudaError_t launch_tiles(const uq_mx &a, const uq_mx &b, ProductArgs p, cudaStream_t st)
 {
     using S = ProductShape<NT>;
@@ -476,9 +504,7 @@ template <int NT, int DT> cudaError_t launch_tiles(const uq_mx &a, const uq_mx &
     if (!codes_map(&map_a, a, NT) || !codes_map(&map_b, b, kRows)) return cudaErrorInvalidValue;
     cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
     const int64_t tiles = (p.n + kRows - 1) / kRows * ((p.m + NT - 1) / NT), stages = (p.k + kStageK - 1) / kStageK;
-    // more CTAs per tile while that still leaves an SM each, and two stages
-    p.split = 1;
-    while (p.split < 8 && tiles * p.split * 2 <= 148 && stages >= p.split * 4) p.split *= 2;
+    p.split = best_split(NT, tiles, stages);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * p.split));
     cfg.blockDim = dim3(kPThreads);

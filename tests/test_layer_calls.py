@@ -121,3 +121,26 @@ def test_the_binding_refuses_shapes_and_types():
         B.uq_layer_norm(f(1, 100).expand(4, 100), None, None, 1e-5, f(4, 100))
     with pytest.raises(ValueError, match="gamma|CUDA"):
         B.uq_layer_norm(f(4, 100), f(99), None, 1e-5, f(4, 100))
+
+
+def test_the_layer_refuses():
+    from paper_2109_12497_b200.layers import NormLinear
+    with pytest.raises(ValueError, match="at least one"):
+        NormLinear(0, 10, 10)
+    with pytest.raises(ValueError, match="float32 or bfloat16"):
+        NormLinear(1, 10, 10, torch.float16)
+    layer = NormLinear(4, 10, 6, device="cpu")               # (its buffers alone; no call is made)
+    assert layer.size == 2 * 10 + 60 and layer.segments() == [0, 10, 20, 80]
+    x = torch.zeros(4, 10, dtype=torch.bfloat16)
+    with pytest.raises(RuntimeError, match="no parameters"):
+        layer.forward(x)
+    with pytest.raises(ValueError, match="theta must be float32"):
+        layer.load(torch.zeros(80, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match=">= 80"):
+        layer.load(torch.zeros(79))
+    layer.gamma = torch.ones(10)
+    for rows in (0, 5):
+        with pytest.raises(ValueError, match="1 to 4 rows"):
+            layer.infer(torch.zeros(rows, 10, dtype=torch.bfloat16))
+    with pytest.raises(ValueError, match="grad must be"):
+        layer.backward(x, torch.zeros(4, 6, dtype=torch.bfloat16), torch.zeros(70), 0)
