@@ -105,7 +105,9 @@ template <int DT, int MAP, int PE> __device__ __forceinline__ void load_piece(co
             if constexpr (DT == UQ_BF16) return __uint_as_float((uint32_t)*(const unsigned short *)(row + i * 2) << 16);
             else return *(const float *)(row + i * 4);
         };
-        if (at + (PE - 1) * piece_step<MAP>() < cols) {    // (all but the last pieces: no questions asked)
+        // all but a row's last pieces without questions: 16384 x 8191 forward 167 -> 147 us (binary32, with half the elements to a
+        // piece, loses by the second copy of the code)
+        if (DT == UQ_BF16 && at + (PE - 1) * piece_step<MAP>() < cols) {
 #pragma unroll
             for (int t = 0; t < PE; ++t) v[t] = element(at + t * piece_step<MAP>());
         } else {
@@ -121,9 +123,6 @@ template <int DT, int MAP, int PE> __device__ __forceinline__ void store_piece(v
         *(float4 *)((float *)row + at) = make_float4(v[0], v[1], v[2], v[3]);
     } else if constexpr (is_wide(MAP)) {
         store8<DT>(row, at, 8, true, v);
-    } else if (at + (PE - 1) * piece_step<MAP>() < cols) {
-#pragma unroll
-        for (int t = 0; t < PE; ++t) store1<DT>(row, at + t * piece_step<MAP>(), v[t]);
     } else {
 #pragma unroll
         for (int t = 0; t < PE; ++t)

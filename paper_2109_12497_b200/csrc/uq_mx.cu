@@ -57,7 +57,7 @@ __device__ __forceinline__ uint4 draw_row(const PhiloxKey &k, const DrawColumn &
     return make_uint4(c0, c1, c2, c3);
 }
 
-// Eight neighbours of a row of the tile in shared memory, and back.
+// Eight neighbours of a row into the tile in shared memory.
 template <int DT> __device__ __forceinline__ void keep_eight(unsigned char *tile, int r, int chunk, const Eight<DT> &x)
 {
     if constexpr (DT == UQ_BF16) {
@@ -70,20 +70,62 @@ template <int DT> __device__ __forceinline__ void keep_eight(unsigned char *tile
         *(uint4 *)(tile + word_at(r, chunk * 8 + (second ? 0 : 4))) = second ? a : b;
     }
 }
-template <int DT> __device__ __forceinline__ void kept_eight(const unsigned char *tile, int r, int chunk, Eight<DT> &x)
+// Eight values from column `chunk` * 8 of a row's piece in the tile, whatever its alignment; 16 neighbouring lanes take a row's 16
+// chunks.  Memory is read in whole 16-byte granules, what lies beside the row (but inside the matrix) included; the granule behind
+// a lane's own comes from the next lane, and the eight values are cut out of both.  have:
+// values of the chunk that exist; last: the next lane holds nothing of the row.
+template <int DT> __device__ __forceinline__ void load_cut(const char *row, const char *begin, const char *end, int chunk, int have, bool last, Eight<DT> &x)
 {
-    if constexpr (DT == UQ_BF16) {
-        const uint4 q = *(const uint4 *)(tile + granule_at(r, chunk));
-        x.w[0] = q.x; x.w[1] = q.y; x.w[2] = q.z; x.w[3] = q.w;
-    } else {
-        const uint4 q = *(const uint4 *)(tile + word_at(r, chunk * 8)), q2 = *(const uint4 *)(tile + word_at(r, chunk * 8 + 4));
-        x.w[0] = q.x; x.w[1] = q.y; x.w[2] = q.z; x.w[3] = q.w;
-        x.w[4] = q2.x; x.w[5] = q2.y; x.w[6] = q2.z; x.w[7] = q2.w;
+    constexpr int E = Elem<DT>::BYTES, W = 2 * E;          // words of a chunk
+    const char *at = row + chunk * 8 * E;
+    const int off = (int)((uintptr_t)row & 15);            // the same for all chunks of the row
+    const char *first = at - off;
+    const auto granule = [&](const char *g) {
+        if (g >= begin && g + 16 <= end) return __ldg((const uint4 *)g);
+        uint32_t w[4] = {};
+        for (int k = 0; k < 16; k += E) {                  // the matrix's first or last granule
+            if (g + k < begin || g + k + E > end) continue;
+            if constexpr (DT == UQ_BF16) {
+                const uint32_t v = __ldg((const unsigned short *)(g + k)) << (8 * (k & 2));
+                if (k < 4) w[0] |= v; else if (k < 8) w[1] |= v; else if (k < 12) w[2] |= v; else w[3] |= v;
+            } else {
+                const uint32_t v = __ldg((const uint32_t *)(g + k));
+                if (k == 0) w[0] = v; else if (k == 4) w[1] = v; else if (k == 8) w[2] = v; else w[3] = v;
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    };
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    uint32_t w[W + 4];
+    const uint4 g0 = have > 0 ? granule(first) : zero;
+    w[0] = g0.x; w[1] = g0.y; w[2] = g0.z; w[3] = g0.w;
+    if constexpr (DT == UQ_F32) {
+        const uint4 g1 = have > 0 && off + 4 * have > 16 ? granule(first + 16) : zero;
+        w[4] = g1.x; w[5] = g1.y; w[6] = g1.z; w[7] = g1.w;
+    }
+    // the next lane's first granule; the last lane reads it itself
+    uint4 g2 = zero;
+    if (last && have > 0 && off + E * have > 4 * W) g2 = granule(first + 4 * W);
+    const uint32_t n0 = __shfl_down_sync(0xFFFFFFFFu, w[0], 1, 16), n1 = __shfl_down_sync(0xFFFFFFFFu, w[1], 1, 16);
+    const uint32_t n2 = __shfl_down_sync(0xFFFFFFFFu, w[2], 1, 16), n3 = __shfl_down_sync(0xFFFFFFFFu, w[3], 1, 16);
+    w[W] = last ? g2.x : n0; w[W + 1] = last ? g2.y : n1; w[W + 2] = last ? g2.z : n2; w[W + 3] = last ? g2.w : n3;
+    // words off / 4 .. of it, a half on if off is odd in words
+#pragma unroll
+    for (int t = 0; t < W + 2; ++t) w[t] = off & 8 ? w[t + 2] : w[t];
+#pragma unroll
+    for (int t = 0; t < W + 1; ++t) w[t] = off & 4 ? w[t + 1] : w[t];
+#pragma unroll
+    for (int t = 0; t < W; ++t) x.w[t] = DT == UQ_BF16 && (off & 2) ? __funnelshift_r(w[t], w[t + 1], 16) : w[t];
+    if (have < 8) {
+#pragma unroll
+        for (int t = 0; t < W; ++t) {
+            if constexpr (DT == UQ_BF16) x.w[t] = 2 * t + 1 < have ? x.w[t] : 2 * t < have ? x.w[t] & 0xFFFFu : 0u;
+            else x.w[t] = t < have ? x.w[t] : 0u;
+        }
     }
 }
 
-// WIDE: rows start on 16 bytes and consist of whole groups of eight; otherwise the tile is fetched element by element, a warp's
-// lanes side by side.
+// WIDE: rows start on 16 bytes and consist of whole groups of eight.
 template <int DT, bool SR, bool WIDE>
 __global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__restrict__ x, int64_t rows, int64_t cols, int64_t ld,
                                                                   const PhiloxKey key, const uq_mx q, const uq_mx qt, uint32_t *status)
@@ -97,23 +139,11 @@ __global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__
     const int64_t tr = blockIdx.x / ktq, tc = blockIdx.x % ktq, r0 = tr * kMxTile, c0 = tc * kMxTile;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rows_here = (int)min((int64_t)kMxTile, rows - r0), cols_here = (int)min((int64_t)kMxTile, cols - c0);
+    const char *end = (const char *)x + ((rows - 1) * ld + cols) * E;
     bool bad = false;
 
     const int chunk = tid & 15, first = tid >> 4;          // eight columns, of every 16th row
-    if constexpr (!WIDE) {
-        for (int r = warp; r < kMxTile; r += kQThreads / 32) {
-            const char *row = (const char *)x + ((r0 + r) * ld + c0) * E;
-#pragma unroll
-            for (int c = lane; c < kMxTile; c += 32) {
-                const bool in = r < rows_here && c < cols_here;
-                if constexpr (DT == UQ_BF16)
-                    *(unsigned short *)(tile + granule_at(r, c >> 3) + (c & 7) * 2) = in ? __ldg((const unsigned short *)row + c) : (unsigned short)0;
-                else
-                    *(float *)(tile + word_at(r, c)) = in ? __ldg((const float *)row + c) : 0.0f;
-            }
-        }
-        __syncthreads();
-    }
+    const int have = max(0, min(8, cols_here - chunk * 8));
     const DrawColumn mine = draw_column(key, (uint32_t)((c0 >> 3) + chunk));
 #pragma unroll 1
     for (int batch = 0; batch < 8; batch += BATCH) {
@@ -131,7 +161,8 @@ __global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__
                 v[k].w[0] = a.x; v[k].w[1] = a.y; v[k].w[2] = a.z; v[k].w[3] = a.w;
                 if constexpr (DT == UQ_F32) { v[k].w[4] = b.x; v[k].w[5] = b.y; v[k].w[6] = b.z; v[k].w[7] = b.w; }
             } else {
-                kept_eight<DT>(tile, r, chunk, v[k]);
+                load_cut<DT>((const char *)x + ((r0 + r) * ld + c0) * E, (const char *)x, end, chunk, r < rows_here ? have : 0,
+                             chunk == 15 || chunk * 8 + 8 >= cols_here, v[k]);
             }
         }
 #pragma unroll
@@ -140,7 +171,7 @@ __global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__
             uint4 h = make_uint4(0, 0, 0, 0);
             if constexpr (SR) h = draw_row(key, mine, (uint32_t)(r0 + r));
             if (along_cols) {
-                if constexpr (WIDE) keep_eight<DT>(tile, r, chunk, v[k]);
+                keep_eight<DT>(tile, r, chunk, v[k]);
                 if constexpr (SR) *(uint4 *)(draws + granule_at(r, chunk)) = h;
             }
             if (along_rows) {
@@ -302,8 +333,7 @@ void launch_tile(const void *x, int64_t rows, int64_t cols, int64_t ld, const Ph
                  uint32_t *status, cudaStream_t st)
 {
     const bool wide = ((uintptr_t)x & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0 && (cols & 7) == 0;
-    const bool tile = !wide || qt.codes != nullptr;
-    const size_t smem = 1024 + (tile ? kTileBytes<DT> + (SR && qt.codes != nullptr ? kHalfTile : 0) : 0);
+    const size_t smem = 1024 + (qt.codes != nullptr ? kTileBytes<DT> + (SR ? kHalfTile : 0) : 0);
     auto kernel = wide ? quantize_tile_kernel<DT, SR, true> : quantize_tile_kernel<DT, SR, false>;
     if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     launch_k_smem(kernel, dim3((unsigned)(mx_ktiles(cols) * mx_ktiles(rows))), dim3(kQThreads), smem, st, x, rows, cols, ld, key, q, qt,
