@@ -18,8 +18,7 @@ constexpr int kQThreads = 256;
 // bytes and 32 more after eight rows, for the same reason (a warp reads eight columns of four rows, eight rows apart).
 __device__ __forceinline__ uint32_t granule_at(int row, int granule) { return row * 256 + ((granule ^ (((row >> 3) & 3) * 2 + (row & 1))) << 4); }
 __device__ __forceinline__ uint32_t word_at(int row, int col) { return (row * 132 + (row >> 3) * 8 + col) * 4; }
-constexpr int kHalfTile = 128 * 256, kWordTile = (128 * 132 + 16 * 8) * 4;
-template <int DT> constexpr int kTileBytes = DT == UQ_BF16 ? kHalfTile : kWordTile;
+template <int DT, int TR> constexpr int kTileBytes = DT == UQ_BF16 ? TR * 256 : (TR * 132 + TR / 8 * 8) * 4;
 
 // Eight rows (8 q .. 8 q + 7 of the 32 from `row` on, for q = lane % 4) of column `granule` * 8 + lane / 4 of a 16-bit tile, in
 // pairs: matrix i holds rows 2 i and 2 i + 1 of each group of eight.
@@ -125,20 +124,21 @@ template <int DT> __device__ __forceinline__ void load_cut(const char *row, cons
     }
 }
 
-// WIDE: rows start on 16 bytes and consist of whole groups of eight.
-template <int DT, bool SR, bool WIDE>
-__global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__restrict__ x, int64_t rows, int64_t cols, int64_t ld,
+// WIDE: rows start on 16 bytes and consist of whole groups of eight.  TR: rows of x per CTA, a whole tile or a quarter of one (where
+// there are few tiles).
+template <int DT, bool SR, bool WIDE, int TR>
+__global__ void __launch_bounds__(kQThreads, SR ? 3 : DT == UQ_BF16 && WIDE ? 5 : 4) quantize_tile_kernel(const void *__restrict__ x, int64_t rows, int64_t cols, int64_t ld,
                                                                   const PhiloxKey key, const uq_mx q, const uq_mx qt, uint32_t *status)
 {
-    constexpr int E = Elem<DT>::BYTES, BATCH = DT == UQ_BF16 ? 8 : 4;
+    constexpr int E = Elem<DT>::BYTES, BATCH = TR == 32 ? 2 : DT == UQ_BF16 ? 8 : 4;
     extern __shared__ __align__(16) unsigned char smem[];
     const bool along_rows = q.codes != nullptr, along_cols = qt.codes != nullptr;
-    unsigned char *scales_q = smem, *scales_t = smem + 512, *tile = smem + 1024, *draws = tile + kTileBytes<DT>;
+    unsigned char *scales_q = smem, *scales_t = smem + 512, *tile = smem + 1024, *draws = tile + kTileBytes<DT, TR>;
     grid_dependency_prologue();
     const int64_t ktq = mx_ktiles(cols), ktt = mx_ktiles(rows);
-    const int64_t tr = blockIdx.x / ktq, tc = blockIdx.x % ktq, r0 = tr * kMxTile, c0 = tc * kMxTile;
+    const int64_t tc = blockIdx.x % ktq, r0 = blockIdx.x / ktq * TR, tr = r0 / kMxTile, c0 = tc * kMxTile;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rows_here = (int)min((int64_t)kMxTile, rows - r0), cols_here = (int)min((int64_t)kMxTile, cols - c0);
+    const int rows_here = (int)min((int64_t)TR, rows - r0), cols_here = (int)min((int64_t)kMxTile, cols - c0);
     const char *end = (const char *)x + ((rows - 1) * ld + cols) * E;
     bool bad = false;
 
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__
     const int have = max(0, min(8, cols_here - chunk * 8));
     const DrawColumn mine = draw_column(key, (uint32_t)((c0 >> 3) + chunk));
 #pragma unroll 1
-    for (int batch = 0; batch < 8; batch += BATCH) {
+    for (int batch = 0; batch < TR / 16; batch += BATCH) {
         Eight<DT> v[BATCH];
 #pragma unroll
         for (int k = 0; k < BATCH; ++k) {
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__
             const int col = g * 8 + group;
             unsigned char *out = qt.codes + (c0 + col) * qt.code_stride + r0 / 2 + part * 4;
 #pragma unroll
-            for (int blk = 0; blk < 4; ++blk) {
+            for (int blk = 0; blk < TR / 32; ++blk) {
                 Eight<DT> v;
                 uint4 h = make_uint4(0, 0, 0, 0);
                 if constexpr (DT == UQ_BF16) {
@@ -213,8 +213,18 @@ __global__ void __launch_bounds__(kQThreads) quantize_tile_kernel(const void *__
         }
         __syncthreads();
     }
-    if (along_rows && warp == 0) *(uint4 *)(q.scales + (tr * ktq + tc) * 512 + lane * 16) = *(const uint4 *)(scales_q + lane * 16);
-    if (along_cols && warp == 1) *(uint4 *)(qt.scales + (tc * ktt + tr) * 512 + lane * 16) = *(const uint4 *)(scales_t + lane * 16);
+    uint8_t *to_q = q.scales + (tr * ktq + tc) * 512, *to_t = qt.scales + (tc * ktt + tr) * 512;
+    if constexpr (TR == kMxTile) {
+        if (along_rows && warp == 0) *(uint4 *)(to_q + lane * 16) = *(const uint4 *)(scales_q + lane * 16);
+        if (along_cols && warp == 1) *(uint4 *)(to_t + lane * 16) = *(const uint4 *)(scales_t + lane * 16);
+    } else {                                               // four bytes of 32 rows, a byte of 128 columns
+        const int quarter = (int)(r0 / 32) & 3;
+        if (along_rows && warp == 0) *(uint32_t *)(to_q + lane * 16 + quarter * 4) = *(const uint32_t *)(scales_q + lane * 16);
+        if (along_cols && warp >= 4) {
+            const int col = tid - 128, at = (col & 31) * 16 + (col >> 5) * 4;
+            to_t[at + quarter] = scales_t[at];
+        }
+    }
     if (status != nullptr && bad) atomicOr(status, UQ_STATUS_NONFINITE);
 }
 
@@ -328,16 +338,24 @@ __global__ void __launch_bounds__(kQThreads) dequantize_kernel(const uq_mx q, vo
     }
 }
 
+// A CTA takes a quarter of a tile where there are few tiles (bf16, both ways, stochastic: 1023 x 2037 11.7 -> 7.0 us, 2048 x 2048
+// 12.8 -> 9.5, 2048 x 4096 17.3 -> 17.6, 4096 x 4096 28.5 -> 33.6), and wherever binary32 columns go through shared memory, whose
+// whole tile leaves an SM few CTAs (4096 x 4096 41.9 -> 37.9 us, 16384 x 8192 340 -> 294; rows alone 146 -> 183).
+constexpr int64_t kQuarterTiles = 300;
+
 template <int DT, bool SR>
 void launch_tile(const void *x, int64_t rows, int64_t cols, int64_t ld, const PhiloxKey &key, const uq_mx &q, const uq_mx &qt,
                  uint32_t *status, cudaStream_t st)
 {
     const bool wide = ((uintptr_t)x & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0 && (cols & 7) == 0;
-    const size_t smem = 1024 + (qt.codes != nullptr ? kTileBytes<DT> + (SR ? kHalfTile : 0) : 0);
-    auto kernel = wide ? quantize_tile_kernel<DT, SR, true> : quantize_tile_kernel<DT, SR, false>;
+    const int64_t tiles = mx_ktiles(cols) * mx_ktiles(rows);
+    const bool small = tiles <= kQuarterTiles || (DT == UQ_F32 && qt.codes != nullptr && 4 * tiles <= 0x7FFFFFFF);
+    const size_t tile = small ? kTileBytes<DT, 32> + (SR ? kTileBytes<UQ_BF16, 32> : 0) : kTileBytes<DT, 128> + (SR ? kTileBytes<UQ_BF16, 128> : 0);
+    const size_t smem = 1024 + (qt.codes != nullptr ? tile : 0);
+    auto kernel = small ? (wide ? quantize_tile_kernel<DT, SR, true, 32> : quantize_tile_kernel<DT, SR, false, 32>)
+                        : (wide ? quantize_tile_kernel<DT, SR, true, 128> : quantize_tile_kernel<DT, SR, false, 128>);
     if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    launch_k_smem(kernel, dim3((unsigned)(mx_ktiles(cols) * mx_ktiles(rows))), dim3(kQThreads), smem, st, x, rows, cols, ld, key, q, qt,
-                  status);
+    launch_k_smem(kernel, dim3((unsigned)(small ? 4 * tiles : tiles)), dim3(kQThreads), smem, st, x, rows, cols, ld, key, q, qt, status);
 }
 
 }  // namespace
