@@ -462,7 +462,8 @@ int uq_randk_update(int64_t d, int64_t K, const int64_t *sel, const float *vals,
  *           code_stride a multiple of 16 and >= 16*ceil(cols/32); the last block's missing values are zeros
  *   scales  uq_mx_scale_bytes(rows, cols) bytes, 16-byte aligned: tiles of 128 rows x 4 blocks (512 bytes), the tiles of
  *           128 rows one after the other; row r and block b of a tile at byte (r%32)*16 + (r/32)*4 + b.  Blocks of a row
- *           beyond its last are written as 0, scales of rows beyond the last are unspecified.
+ *           beyond its last are written as 0 (a product wants none of them to be NaN), scales of rows beyond the last are
+ *           unspecified and not looked at.
  */
 typedef struct uq_mx {
     int64_t rows, cols;

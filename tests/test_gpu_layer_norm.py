@@ -24,6 +24,10 @@ def inputs(rows, cols, seed):
     return x, gamma, beta, dy
 
 
+def f64(t):
+    return t.double().cpu().numpy()
+
+
 def cuda(v):
     return None if v is None else torch.from_numpy(v).cuda()
 
@@ -226,3 +230,47 @@ def test_in_graphs_that_share_a_workspace_and_on_streams():
             graph.replay()
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements: the last rows are those of the same rows by themselves, and the sums over the rows are whole."""
+    rows, cols = 262_200, 8_192
+    x = torch.full((rows, cols), 0.5, dtype=torch.bfloat16, device="cuda")
+    x[:, ::2] = -0.25
+    x[-4:] = torch.randn(4, cols, device="cuda").bfloat16()
+    gamma, beta = torch.rand(cols, device="cuda") + 0.5, torch.randn(cols, device="cuda")
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    B.uq_layer_norm(x, gamma, beta, EPS, y, mean, rstd)
+    small = torch.empty(4, cols, dtype=torch.bfloat16, device="cuda")
+    B.uq_layer_norm(x[-4:], gamma, beta, EPS, small)
+    assert torch.equal(y[-4:], small)
+    dy = torch.ones_like(x)
+    dg, db = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+    ws = torch.empty(B.uq_layer_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    B.uq_layer_norm_backward(dy, x, gamma, mean, rstd, y, dg, db, ws)
+    assert (db == rows).all()                                # sums of ones below 2^24: exact
+    one = torch.empty(4, cols, dtype=torch.bfloat16, device="cuda")
+    B.uq_layer_norm_backward(dy[-4:], x[-4:], gamma, mean[-4:], rstd[-4:], one, None, None, ws)
+    assert torch.equal(y[-4:], one)
+
+
+def test_two_backward_passes_at_once():
+    """Two streams, a workspace each."""
+    rows, cols = 300, 2500
+    runs = []
+    for k in range(2):
+        x, gamma, _, dy = inputs(rows, cols, 20 + k)
+        t, d, g = as_matrix(x, torch.float32, 1, 1), as_matrix(dy, torch.float32), cuda(gamma)
+        mean, rstd = (cuda(v.astype(np.float32)) for v in ref.layer_norm(f64(t), None, None, EPS)[1:])
+        outs = [torch.empty(rows, cols, device="cuda"), torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")]
+        ws = torch.empty(B.uq_layer_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+        B.uq_layer_norm_backward(d, t, g, mean, rstd, *outs, ws)
+        runs.append((d, t, g, mean, rstd, outs, ws, [o.clone() for o in outs], torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for d, t, g, mean, rstd, outs, ws, _, stream in runs:
+            with torch.cuda.stream(stream):
+                B.uq_layer_norm_backward(d, t, g, mean, rstd, *outs, ws)
+    torch.cuda.synchronize()
+    for *_, outs, _, want, _ in runs:
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))

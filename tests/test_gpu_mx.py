@@ -267,7 +267,7 @@ def test_product_carries_nan_scales_to_their_row_and_column_only():
 
 def test_product_does_not_read_what_is_not_the_matrix():
     """Scales of rows behind the last and bytes between the rows of codes may hold anything, NaN scales among it."""
-    for m, n, k in ((5, 9, 100), (130, 200, 300)):
+    for m, n, k in ((5, 9, 100), (130, 200, 300), (2100, 2300, 650)):
         a, va = random_mx(m, k, 3, 127, 128)
         b, vb = random_mx(n, k, 4, 127, 128)
         def poisoned(x, rows):
@@ -335,3 +335,30 @@ def test_two_streams_at_once():
         want = a[1] @ b[1].T
         for o in outs:
             assert np.array_equal(o[j].double().cpu().numpy(), want)
+
+
+def test_offsets_beyond_32_bits():
+    """Matrices of more than 2^31 elements: the last rows are those of the same rows by themselves."""
+    rows, cols = 131_080, 16_640
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x.copy_(torch.arange(cols, device="cuda").remainder(997).sub(498).bfloat16().expand(rows, cols))
+    x[-8:] = torch.randn(8, cols, device="cuda").bfloat16()
+    q, last = B.MxMatrix(rows, cols), B.MxMatrix(8, cols)
+    B.uq_mx_quantize(x, 0, 0, q, None, None)
+    B.uq_mx_quantize(x[-8:], 0, 0, last, None, None)
+    assert torch.equal(q.codes[-8:], last.codes)
+    want = torch.empty(8, cols, dtype=torch.bfloat16, device="cuda")
+    B.uq_mx_dequantize(last, want)
+    B.uq_mx_dequantize(q, x)                                 # over its own input: the calls are in order
+    assert torch.equal(x[-8:], want)
+    del x, q
+    n = 46_400                                               # n * n > 2^31, by pairs of CTAs; and few rows of a long out
+    (a, va), (b, vb) = random_mx(64, 96, 1, 127, 128), random_mx(64, 96, 2, 127, 128)
+    big = lambda m: B.MxMatrix(n, 96, m.codes.repeat(n // 64, 1), m.scales.repeat(-(-n // 128)))
+    a.scales.view(-1, 32, 4, 4)[:, :, 2:] = a.scales.view(-1, 32, 4, 4)[:, :, :2]        # 64 rows twice in a tile of 128
+    b.scales.view(-1, 32, 4, 4)[:, :, 2:] = b.scales.view(-1, 32, 4, 4)[:, :, :2]
+    out = torch.empty(n, n, dtype=torch.bfloat16, device="cuda")
+    B.uq_mx_product(big(a), big(b), out, None, None)
+    want = torch.from_numpy(va @ vb.T).float().bfloat16().cuda()
+    for i in (0, n // 2 // 64 * 64, n - 64):
+        assert torch.equal(out[i:i + 64, -64:], want) and torch.equal(out[i:i + 64, :64], want)
