@@ -623,16 +623,20 @@ def uq_mx_quantize(x: torch.Tensor, seed: int, rng_bits: int, q: Optional[MxMatr
     device = x.get_device()
     (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
     px, ld = _matrix(x, rows, cols, x.dtype, device, "x")
-    _check("uq_mx_quantize", lib().uq_mx_quantize(
+    rc = (_lib or lib()).uq_mx_quantize(
         px, rows, cols, ld, dtype, seed & 0xFFFFFFFFFFFFFFFF, rng_bits, None if q is None else q.ref(device),
-        None if qt is None else qt.ref(device), _status(status, device), _stream_of(device)))
+        None if qt is None else qt.ref(device), _status(status, device), _stream_of(device))
+    if rc:
+        raise UqError("uq_mx_quantize", rc)
 
 
 def uq_mx_dequantize(q: MxMatrix, out: torch.Tensor) -> None:
     """The values that a microscaled matrix stands for (exact in either type)."""
     device = out.get_device()
     dtype, (po, ld) = _dtype(out, "out"), _matrix(out, q.rows, q.cols, out.dtype, device, "out")
-    _check("uq_mx_dequantize", lib().uq_mx_dequantize(q.ref(device), po, ld, dtype, _stream_of(device)))
+    rc = (_lib or lib()).uq_mx_dequantize(q.ref(device), po, ld, dtype, _stream_of(device))
+    if rc:
+        raise UqError("uq_mx_dequantize", rc)
 
 
 def uq_mx_product(a: MxMatrix, b: MxMatrix, out: torch.Tensor, add: Optional[torch.Tensor] = None,
@@ -643,8 +647,10 @@ def uq_mx_product(a: MxMatrix, b: MxMatrix, out: torch.Tensor, add: Optional[tor
     device = out.get_device()
     dtype, (po, ld) = _dtype(out, "out"), _matrix(out, a.rows, b.rows, out.dtype, device, "out")
     pa, add_ld = (None, 0) if add is None else _matrix(add, a.rows, b.rows, out.dtype, device, "add")
-    _check("uq_mx_product", lib().uq_mx_product(a.ref(device), b.ref(device), pa, add_ld, po, ld, dtype, _status(status, device),
-                                                _stream_of(device)))
+    rc = (_lib or lib()).uq_mx_product(a.ref(device), b.ref(device), pa, add_ld, po, ld, dtype, _status(status, device),
+                                                _stream_of(device))
+    if rc:
+        raise UqError("uq_mx_product", rc)
 
 
 def uq_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float,
@@ -655,10 +661,12 @@ def uq_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional
     (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
     px, ld = _matrix(x, rows, cols, x.dtype, device, "x")
     py, y_ld = (None, 0) if y is None else _matrix(y, rows, cols, x.dtype, device, "y")
-    _check("uq_layer_norm", lib().uq_layer_norm(
+    rc = (_lib or lib()).uq_layer_norm(
         px, rows, cols, ld, dtype, _vector(gamma, cols, device, "gamma"), _vector(beta, cols, device, "beta"), eps, py, y_ld,
         _vector(mean, rows, device, "mean"), _vector(rstd, rows, device, "rstd"), None if q is None else q.ref(device),
-        _status(status, device), _stream_of(device)))
+        _status(status, device), _stream_of(device))
+    if rc:
+        raise UqError("uq_layer_norm", rc)
 
 
 def uq_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
@@ -682,8 +690,10 @@ def uq_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[to
     index = workspace.get_device()
     if index != device:
         _refuse_device(index, device, "the workspace")
-    _check("uq_layer_norm_backward", lib().uq_layer_norm_backward(
+    rc = (_lib or lib()).uq_layer_norm_backward(
         pdy, dy_ld, px, x_ld, rows, cols, dtype, _vector(gamma, cols, device, "gamma"), _vector(mean, rows, device, "mean"),
         _vector(rstd, rows, device, "rstd"), pdx, dx_ld, _vector(dgamma, cols, device, "dgamma", grad_dtype),
         _vector(dbeta, cols, device, "dbeta", grad_dtype), UQ_F32 if grad is None else _dtype(grad, "dgamma and dbeta"),
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_of(device)))
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_of(device))
+    if rc:
+        raise UqError("uq_layer_norm_backward", rc)

@@ -70,12 +70,15 @@ template <int B> __device__ __forceinline__ uint32_t same_byte(uint32_t w0, uint
     return __byte_perm(__byte_perm(w0, w1, sel), __byte_perm(w2, w3, sel), 0x5410);
 }
 
-// Magnitude codes (bits 16 to 18 of `code`; what lies above and below is not defined) of two values of magnitude a * inv in
-// [0, 6], rounded up iff h < rint(p * 2^16).  The codes' values 0, 0.5 .. 2, 3, 4, 6 are the places where a concave function of
-// three pieces takes whole numbers: with a' = a * inv it is half of min(2 a', a' + 2, a' / 2 + 4) (slopes 2, 1, 1/2 up to 2, 4, 6).
-// Each piece plus 64 is one fused multiply-add with a single rounding, to 2^-17, ties to even: the minimum's low bits are
-// code * 2^16 + rint(p * 2^16).  2^16 - 1 - h carries into the code iff h is below the fraction.
-__device__ __forceinline__ void e2m1_stochastic_pair(float a0, float a1, float inv, uint32_t h0, uint32_t h1, uint32_t &code0, uint32_t &code1)
+// Magnitude codes (bits 0 to 2 of `code`; what lies above is a constant) of two values of magnitude a * inv in [0, 6], rounded up
+// iff h < rint(p * 2^16); `draws` holds the two h.  The codes' values 0, 0.5 .. 2, 3, 4, 6 are the places where a concave function
+// of three pieces takes whole numbers: with a' = a * inv it is half of min(2 a', a' + 2, a' / 2 + 4) (slopes 2, 1, 1/2 up to 2, 4,
+// 6).  Each piece plus 64 is one fused multiply-add with a single rounding, to 2^-17, ties to even: the minimum is
+// 64 + (code + rint(p * 2^16) / 2^16) / 2.  A draw put into the mantissa of 64 is 64 + h / 2^17; the difference is exact, and
+// rounding it up to a multiple of one half (the last place of 2^22 + 64, which a difference
+// down to -1/2 does not leave) rounds the code up iff h is below the fraction.  (Integer
+// additions and shifts in place of the last two steps take 1 to 2 % longer: the integer pipe, which gathers and masks, is the busier.)
+__device__ __forceinline__ void e2m1_stochastic_pair(float a0, float a1, float inv, uint32_t draws, uint32_t &code0, uint32_t &code1)
 {
     float s0, s1, t0, t1, u0, u1;
     fma_pair(a0, a1, inv, 64.0f, s0, s1);
@@ -83,8 +86,14 @@ __device__ __forceinline__ void e2m1_stochastic_pair(float a0, float a1, float i
     fma_pair(a0, a1, 0.25f * inv, 66.0f, u0, u1);
     asm("min.f32 %0, %0, %1, %2;" : "+f"(s0) : "f"(t0), "f"(u0));
     asm("min.f32 %0, %0, %1, %2;" : "+f"(s1) : "f"(t1), "f"(u1));
-    code0 = __float_as_uint(s0) + 65535u - h0;             // 64 has no bits below bit 23
-    code1 = __float_as_uint(s1) + 65535u - h1;
+    const uint32_t h0 = __byte_perm(draws, 0x42800000u, 0x7610), h1 = __byte_perm(draws, 0x42800000u, 0x7632);
+    uint64_t x, y, r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(s0), "f"(s1));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "r"(h0), "r"(h1));
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
+    asm("mov.b64 %0, {%1, %1};" : "=l"(y) : "f"(4194368.0f));
+    asm("add.rp.f32x2 %0, %1, %2;" : "=l"(r) : "l"(r), "l"(y));
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(code0), "=r"(code1) : "l"(r));
 }
 
 // Eight neighbouring values as they lie in memory.
@@ -151,8 +160,8 @@ template <int DT, bool SR> __device__ __forceinline__ uint32_t quantize_eight(co
         uint32_t c[8];
         x.magnitudes(v);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) e2m1_stochastic_pair(v[2 * t], v[2 * t + 1], inv, h[t] & 0xFFFFu, h[t] >> 16, c[2 * t], c[2 * t + 1]);
-        const uint32_t even = same_byte<2>(c[0], c[2], c[4], c[6]), odd = same_byte<2>(c[1], c[3], c[5], c[7]);
+        for (int t = 0; t < 4; ++t) e2m1_stochastic_pair(v[2 * t], v[2 * t + 1], inv, h[t], c[2 * t], c[2 * t + 1]);
+        const uint32_t even = same_byte<0>(c[0], c[2], c[4], c[6]), odd = same_byte<0>(c[1], c[3], c[5], c[7]);
         codes = (even & 0x07070707u) | ((x.even_signs() >> 4) & 0x08080808u) | ((odd << 4) & 0x70707070u) | (x.odd_signs() & 0x80808080u);
     } else {
         x.values(v);
