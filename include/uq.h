@@ -9,6 +9,9 @@
  * The M workers are M resident device buffers; the paper's three all-reduces (max of the norm,
  * min of the scale index, sum of the levels) are on-device reductions over those buffers.
  *
+ * Beside it, at the end of this file: the operators of a layer whose weight gradients fill those buffers (microscaled
+ * 4-bit quantization and product, layer norm).
+ *
  * Common rules
  *   - Every data pointer is a DEVICE pointer owned by the caller unless marked "host".
  *     The library allocates no device memory and keeps no state between calls.

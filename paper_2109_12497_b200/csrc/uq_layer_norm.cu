@@ -12,6 +12,8 @@
 // lies beside the row (but inside the matrix) included, and a row keeps its offset from 16 bytes there.  Which elements a
 // thread holds depends on that offset: neighbours in 16-byte accesses, or elements that are 32 apart, so that a warp's scalar
 // accesses are contiguous.
+// Measured at 16384 x 8192: forward bf16 85 us (6.3 TB/s), binary32 186 us (5.8), backward bf16 161 us (5.0), binary32 260 us (6.2); with
+// rows that start anywhere (8191 columns, bf16) 147 and 269 us.
 #include "uq_mx.cuh"
 
 namespace uq {

@@ -75,9 +75,9 @@ template <int B> __device__ __forceinline__ uint32_t same_byte(uint32_t w0, uint
 // of three pieces takes whole numbers: with a' = a * inv it is half of min(2 a', a' + 2, a' / 2 + 4) (slopes 2, 1, 1/2 up to 2, 4,
 // 6).  Each piece plus 64 is one fused multiply-add with a single rounding, to 2^-17, ties to even: the minimum is
 // 64 + (code + rint(p * 2^16) / 2^16) / 2.  A draw put into the mantissa of 64 is 64 + h / 2^17; the difference is exact, and
-// rounding it up to a multiple of one half (the last place of 2^22 + 64, which a difference
-// down to -1/2 does not leave) rounds the code up iff h is below the fraction.  (Integer
-// additions and shifts in place of the last two steps take 1 to 2 % longer: the integer pipe, which gathers and masks, is the busier.)
+// rounding it up to a multiple of one half (the last place of 2^22 + 64, which a difference down to -1/2 does not leave) rounds
+// the code up iff h is below the fraction.  (Integer additions and shifts in place of the last two steps take 1 to 2 % longer: the
+// integer pipe, which gathers and masks, is the busier one.  Single instead of paired multiply-adds: 3 % longer.)
 __device__ __forceinline__ void e2m1_stochastic_pair(float a0, float a1, float inv, uint32_t draws, uint32_t &code0, uint32_t &code1)
 {
     float s0, s1, t0, t1, u0, u1;
