@@ -26,8 +26,9 @@ struct ProductArgs {
 
 constexpr int kRows = 128;                                 // of b per tile
 constexpr int kStageK = 256;                               // columns per stage: 128 bytes of a row
-constexpr int kPThreads = 192;                             // warp 0 copies, warp 1 multiplies, warps 2 to 5 store
-constexpr int kPairThreads = 320;                          // ... warps 2 to 9
+// Warp 0 copies, warp 1 multiplies, the others store: PARTS warps for each quarter of the lanes, taking turns of 16 columns.
+constexpr int kPairParts = 4;
+constexpr int threads_of(int parts) { return 64 + 128 * parts; }
 
 template <int DT> __device__ __forceinline__ float load1(const void *base, int64_t at)
 {
@@ -95,6 +96,7 @@ template <int CTAS, int NT, int A_AT> __device__ __forceinline__ void multiply_s
 template <int NT> struct ProductShape {
     static constexpr int kStageBytes = kRows * 128 + NT * 128 + 2048;
     static constexpr int kStages = NT == 128 ? 3 : NT == 16 ? 5 : 4;      // two CTAs fit an SM
+    static constexpr int kParts = NT >= 64 ? 2 : 1, kThreads = threads_of(kParts);
     static constexpr int kScaleColumns = 16;               // per stage: 2 x 4 of each operand
     static constexpr int kColumns = NT + kStages * kScaleColumns <= 128 ? 128 : 256;
     static constexpr int kSmem = kStages * kStageBytes + 1024 + 256;
@@ -103,7 +105,7 @@ template <int NT> struct ProductShape {
 // A tile of 128 rows of b and NT of a.  With split > 1 the CTAs of a cluster take a share of the columns each, put their sums
 // into shared memory, and each adds up a share of the tile in the CTAs' order.
 template <int NT, int DT>
-__global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+__global__ void __launch_bounds__(ProductShape<NT>::kThreads) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                             const ProductArgs p)
 {
     using S = ProductShape<NT>;
@@ -183,7 +185,7 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
         const int64_t j = n0 + quarter * 32 + lane;
         const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
-        for (int c = 0; c < NT; c += 16) {
+        for (int c = ((warp - 2) >> 2) * 16; c < NT; c += 16 * S::kParts) {
             float v[16];
             __syncwarp();
             tmem_load16(acc + c, v);
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(kPThreads) product_kernel(const __grid_constan
         cluster_sync();
         // Four neighbouring rows of b per thread, from all CTAs in their order; the loads of several columns in flight together.
         const int c0 = NT * (int)rank / p.split, c1 = NT * ((int)rank + 1) / p.split;
-        for (int e = tid; e < (c1 - c0) * (kRows / 4); e += kPThreads) {
+        for (int e = tid; e < (c1 - c0) * (kRows / 4); e += S::kThreads) {
             const int c = c0 + e / (kRows / 4), l = e % (kRows / 4) * 4;
             if (m0 + c >= p.m) continue;
             float4 w[8];
@@ -261,6 +263,7 @@ template <int NT> struct PairShape {
     static constexpr int kScales = 512 - kScaleSlots * kSlotColumns;      // first column of the scales
     static constexpr int kSecond = kScales - NT < NT ? (kScales - NT) / 16 * 16 : NT;   // first column of the second tile's sums
     static constexpr int kShared = NT - kSecond;           // columns that are stored first
+    static_assert(kShared >= 16 * kPairParts && kSecond + NT <= kScales, "each storing warp has a part of the shared columns");
     static constexpr int kSmem = kStages * kStageBytes + 1024 + 256;
 };
 
@@ -274,7 +277,7 @@ __device__ __forceinline__ void tile_place(int64_t t, int64_t tiles_m, int64_t t
 }
 
 template <int NT, int DT>
-__global__ void __launch_bounds__(kPairThreads) __cluster_dims__(2, 1, 1)
+__global__ void __launch_bounds__(threads_of(kPairParts)) __cluster_dims__(2, 1, 1)
 product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                     const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb, const ProductArgs p)
 {
@@ -298,7 +301,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     grid_dependency_trigger();
     if (tid == 0) {
         for (int s = 0; s < 2 * ST + 1; ++s) barrier_init(full + 8 * s, 1);
-        barrier_init(sums_free, 16);                       // eight warps of either CTA
+        barrier_init(sums_free, 8 * kPairParts);           // the storing warps of both CTAs
         barrier_init(drained, 1);
         *gave_up = 0;
         *issued = 0;
@@ -371,8 +374,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             barrier_wait_warp(drained, 0, &again);
         }
     } else if (warp >= 2) {
-        // Two warps for each quarter of the lanes, taking turns of 16 columns.  What is added to a piece is loaded a piece ahead,
-        // the first piece's before the sums are there.
+        // What is added to a piece is loaded a piece ahead, the first piece's before the sums are there.
         const int quarter = warp & 3, part = (warp - 2) >> 2;
         const uint32_t free_bar = cluster_address(sums_free, 0);
         int turn = 0;
@@ -382,7 +384,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             const int64_t j = tn * 256 + rank * 128 + quarter * 32 + lane, m0 = tm * NT;
             const uint32_t sums = tmem + (turn & 1) * S::kSecond + ((uint32_t)(quarter * 32) << 16);
             // the first of two overlapping tiles shares its last columns, the second its first
-            const int first = (turn & 1) || S::kShared == 0 ? 0 : NT - S::kShared;
+            const int first = turn & 1 ? 0 : NT - S::kShared;
             const auto column = [&](int done) { return first + done < NT ? first + done : first + done - NT; };
             const auto rows_there = [&](int c) { return j < p.n ? (int)max((int64_t)0, min((int64_t)16, p.m - m0 - c)) : 0; };
             float w[16];
@@ -390,13 +392,13 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             if (!barrier_wait_warp(sums_ready, turn & 1, gave_up)) break;
             tensor_fence_after();
 #pragma unroll 1
-            for (int done = part * 16; done < NT; done += 32) {
+            for (int done = part * 16; done < NT; done += 16 * kPairParts) {
                 const int c = column(done), have = rows_there(c);
                 float v[16];
                 __syncwarp();
                 tmem_load16(sums + c, v);
                 tmem_load_wait();
-                if (done < (S::kShared == 0 ? NT : S::kShared) && done + 32 >= (S::kShared == 0 ? NT : S::kShared)) {
+                if (done < S::kShared && done + 16 * kPairParts >= S::kShared) {
                     tensor_fence_before();
                     __syncwarp();
                     if (lane == 0) cluster_arrive(free_bar);
@@ -404,8 +406,8 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if (p.add != nullptr) {
 #pragma unroll
                     for (int k = 0; k < 16; ++k) v[k] += w[k];
-                    const int next = column(done + 32 < NT ? done + 32 : done);
-                    if (done + 32 < NT) load_column<DT>(p.add, p.add_ld, m0 + next, j, rows_there(next), w);
+                    const int after = done + 16 * kPairParts, next = column(after < NT ? after : done);
+                    if (after < NT) load_column<DT>(p.add, p.add_ld, m0 + next, j, rows_there(next), w);
                 }
                 if (have > 0) store_column<DT>(p.out, p.ld, m0 + c, j, have, v);
             }
@@ -479,7 +481,7 @@ template <int NT, int DT> cudaError_t launch_pairs(const uq_mx &a, const uq_mx &
         return cudaErrorInvalidValue;
     cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
     const int64_t tiles = (p.n + 255) / 256 * ((p.m + NT - 1) / NT);
-    launch_k_smem(kernel, dim3((unsigned)(min(tiles, (int64_t)74) * 2)), dim3(kPairThreads), S::kSmem, st, map_a, map_b, map_sa, map_sb, p);
+    launch_k_smem(kernel, dim3((unsigned)(min(tiles, (int64_t)74) * 2)), dim3(threads_of(kPairParts)), S::kSmem, st, map_a, map_b, map_sa, map_sb, p);
     return cudaGetLastError();
 }
 
@@ -510,7 +512,7 @@ template <int NT, int DT> cudaError_t launch_tiles(const uq_mx &a, const uq_mx &
     p.split = best_split(NT, tiles, stages);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * p.split));
-    cfg.blockDim = dim3(kPThreads);
+    cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
