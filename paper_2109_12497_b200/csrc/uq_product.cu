@@ -42,28 +42,31 @@ template <int DT> __device__ __forceinline__ void store_result(const ProductArgs
     store1<DT>(p.out, i * p.ld + j, v);
 }
 
-// 16 rows of out from row i on, in one column; `have` of them exist.
-template <int DT> __device__ __forceinline__ void load_column(const void *base, int64_t ld, int64_t i, int64_t j, int have, float (&v)[16])
+// 16 rows of out (or of what is added) from row i on, in this lane's column of the 32 from j0 on; `have` of them exist.  The rows'
+// addresses are the same for a warp: they stay in uniform registers, and a lane adds its constant offset.
+template <int DT> __device__ __forceinline__ void load_column(const void *base, int64_t ld, int64_t i, int64_t j0, int lane, int have, float (&v)[16])
 {
-    const char *at = (const char *)base + (i * ld + j) * Elem<DT>::BYTES;
+    const char *row = (const char *)base + (i * ld + j0) * Elem<DT>::BYTES;
+    const uint32_t off = lane * Elem<DT>::BYTES;
     if (have >= 16) {
 #pragma unroll
-        for (int t = 0; t < 16; ++t, at += ld * Elem<DT>::BYTES) v[t] = load1<DT>(at, 0);
+        for (int t = 0; t < 16; ++t, row += ld * Elem<DT>::BYTES) v[t] = load1<DT>(row + off, 0);
     } else {
 #pragma unroll
-        for (int t = 0; t < 16; ++t, at += ld * Elem<DT>::BYTES) v[t] = t < have ? load1<DT>(at, 0) : 0.0f;
+        for (int t = 0; t < 16; ++t, row += ld * Elem<DT>::BYTES) v[t] = t < have ? load1<DT>(row + off, 0) : 0.0f;
     }
 }
-template <int DT> __device__ __forceinline__ void store_column(void *base, int64_t ld, int64_t i, int64_t j, int have, const float (&v)[16])
+template <int DT> __device__ __forceinline__ void store_column(void *base, int64_t ld, int64_t i, int64_t j0, int lane, int have, const float (&v)[16])
 {
-    char *at = (char *)base + (i * ld + j) * Elem<DT>::BYTES;
+    char *row = (char *)base + (i * ld + j0) * Elem<DT>::BYTES;
+    const uint32_t off = lane * Elem<DT>::BYTES;
     if (have >= 16) {
 #pragma unroll
-        for (int t = 0; t < 16; ++t, at += ld * Elem<DT>::BYTES) store1<DT>(at, 0, v[t]);
+        for (int t = 0; t < 16; ++t, row += ld * Elem<DT>::BYTES) store1<DT>(row + off, 0, v[t]);
     } else {
 #pragma unroll
-        for (int t = 0; t < 16; ++t, at += ld * Elem<DT>::BYTES)
-            if (t < have) store1<DT>(at, 0, v[t]);
+        for (int t = 0; t < 16; ++t, row += ld * Elem<DT>::BYTES)
+            if (t < have) store1<DT>(row + off, 0, v[t]);
     }
 }
 
@@ -182,7 +185,7 @@ __global__ void __launch_bounds__(ProductShape<NT>::kThreads) product_kernel(con
         barrier_wait_warp(done, 0, gave_up);
         tensor_fence_after();
         const int quarter = warp & 3;
-        const int64_t j = n0 + quarter * 32 + lane;
+        const int64_t j0 = n0 + quarter * 32;
         const uint32_t acc = tmem + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll 1
         for (int c = ((warp - 2) >> 2) * 16; c < NT; c += 16 * S::kParts) {
@@ -194,15 +197,15 @@ __global__ void __launch_bounds__(ProductShape<NT>::kThreads) product_kernel(con
                 float *sums = (float *)base;               // every stage has been read: [column][lane]
 #pragma unroll
                 for (int t = 0; t < 16; ++t) sums[(c + t) * kRows + quarter * 32 + lane] = v[t];
-            } else if (j < p.n && m0 + c < p.m) {
+            } else if (j0 + lane < p.n && m0 + c < p.m) {
                 const int have = (int)min((int64_t)16, p.m - m0 - c);
                 if (p.add != nullptr) {                    // all of it first: it may be out itself, so no load moves in front of a store
                     float w[16];
-                    load_column<DT>(p.add, p.add_ld, m0 + c, j, have, w);
+                    load_column<DT>(p.add, p.add_ld, m0 + c, j0, lane, have, w);
 #pragma unroll
                     for (int t = 0; t < 16; ++t) v[t] += w[t];
                 }
-                store_column<DT>(p.out, p.ld, m0 + c, j, have, v);
+                store_column<DT>(p.out, p.ld, m0 + c, j0, lane, have, v);
             }
         }
         tensor_fence_before();
@@ -381,14 +384,15 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         for (int64_t t = pair; t < tiles; t += pairs, ++turn) {
             int64_t tm, tn;
             tile_place(t, tiles_m, tiles_n, &tm, &tn);
-            const int64_t j = tn * 256 + rank * 128 + quarter * 32 + lane, m0 = tm * NT;
+            const int64_t j0 = tn * 256 + rank * 128 + quarter * 32, m0 = tm * NT;
             const uint32_t sums = tmem + (turn & 1) * S::kSecond + ((uint32_t)(quarter * 32) << 16);
             // the first of two overlapping tiles shares its last columns, the second its first
             const int first = turn & 1 ? 0 : NT - S::kShared;
             const auto column = [&](int done) { return first + done < NT ? first + done : first + done - NT; };
-            const auto rows_there = [&](int c) { return j < p.n ? (int)max((int64_t)0, min((int64_t)16, p.m - m0 - c)) : 0; };
+            const auto rows_there = [&](int c) { return (int)max((int64_t)0, min((int64_t)16, p.m - m0 - c)); };
+            const bool mine = j0 + lane < p.n;
             float w[16];
-            if (p.add != nullptr) load_column<DT>(p.add, p.add_ld, m0 + column(part * 16), j, rows_there(column(part * 16)), w);
+            if (p.add != nullptr && mine) load_column<DT>(p.add, p.add_ld, m0 + column(part * 16), j0, lane, rows_there(column(part * 16)), w);
             if (!barrier_wait_warp(sums_ready, turn & 1, gave_up)) break;
             tensor_fence_after();
 #pragma unroll 1
@@ -407,9 +411,9 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 #pragma unroll
                     for (int k = 0; k < 16; ++k) v[k] += w[k];
                     const int after = done + 16 * kPairParts, next = column(after < NT ? after : done);
-                    if (after < NT) load_column<DT>(p.add, p.add_ld, m0 + next, j, rows_there(next), w);
+                    if (after < NT && mine) load_column<DT>(p.add, p.add_ld, m0 + next, j0, lane, rows_there(next), w);
                 }
-                if (have > 0) store_column<DT>(p.out, p.ld, m0 + c, j, have, v);
+                if (have > 0 && mine) store_column<DT>(p.out, p.ld, m0 + c, j0, lane, have, v);
             }
         }
     }

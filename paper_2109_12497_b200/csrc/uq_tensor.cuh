@@ -92,10 +92,11 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
-// An arrival at a barrier of any CTA of the cluster.
+// An arrival at a barrier of any CTA of the cluster.  It orders nothing that this thread has written to memory (a release would
+// wait for all its stores): what it says is that tensor memory has been read.
 __device__ __forceinline__ void cluster_arrive(uint32_t bar)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
 }
 __device__ __forceinline__ float4 cluster_load4(uint32_t addr)
 {
