@@ -537,7 +537,9 @@ template <int DT> cudaError_t launch_product(const uq_mx &a, const uq_mx &b, con
     if (p.m <= 16) return launch_tiles<16, DT>(a, b, p, st);
     if (p.m <= 32) return launch_tiles<32, DT>(a, b, p, st);
     if (p.m <= 64) return launch_tiles<64, DT>(a, b, p, st);
-    if ((p.n + 255) / 256 * ((p.m + 255) / 256) >= 74) return launch_pairs<256, DT>(a, b, p, st);
+    // Pairs where there are more tiles of 128 x 128 than SMs (us, pairs against tiles: 700 x 5000 x 3000 9.3 and 11.1, 2000^3 8.9 and
+    // 10.6, 1024 x 4096 x 4096 10.7 and 10.9, 2048 x 2304 x 1024 7.0 and 6.1; with an SM for each tile 512 x 4096 x 4096 10.0 and 7.4).
+    if ((p.n + 127) / 128 * ((p.m + 127) / 128) > 148) return launch_pairs<256, DT>(a, b, p, st);
     return launch_tiles<128, DT>(a, b, p, st);
 }
 
