@@ -70,58 +70,32 @@ template <int DT> __device__ __forceinline__ void keep_eight(unsigned char *tile
         *(uint4 *)(tile + word_at(r, chunk * 8 + (second ? 0 : 4))) = second ? a : b;
     }
 }
-// Eight values from column `chunk` * 8 of a row's piece in the tile, whatever its alignment; 16 neighbouring lanes take a row's 16
-// chunks.  Memory is read in whole 16-byte granules, what lies beside the row (but inside the matrix) included; the granule behind
-// a lane's own comes from the next lane, and the eight values are cut out of both.  have:
-// values of the chunk that exist; last: the next lane holds nothing of the row.
-template <int DT> __device__ __forceinline__ void load_cut(const char *row, const char *begin, const char *end, int chunk, int have, bool last, Eight<DT> &x)
+// Eight values from `at` on, whatever its alignment; `have` of them exist.  bf16: five words that the values touch (what lies beside
+// the row, but inside the matrix, included), cut where a half is over; single values at the matrix's ends and a row's end.  (Whole
+// 16-byte granules, completed by the next lane's, read memory in fewer instructions but cost 20 more on the pipe that bounds the
+// kernel: 8192 x 8191 stochastic both ways 143 us against 131, binary32 175 against 152.)
+template <int DT> __device__ __forceinline__ void load_cut(const char *at, const char *begin, const char *end, int have, Eight<DT> &x)
 {
-    constexpr int E = Elem<DT>::BYTES, W = 2 * E;          // words of a chunk
-    const char *at = row + chunk * 8 * E;
-    const int off = (int)((uintptr_t)row & 15);            // the same for all chunks of the row
-    const char *first = at - off;
-    const auto granule = [&](const char *g) {
-        if (g >= begin && g + 16 <= end) return __ldg((const uint4 *)g);
-        uint32_t w[4] = {};
-        for (int k = 0; k < 16; k += E) {                  // the matrix's first or last granule
-            if (g + k < begin || g + k + E > end) continue;
-            if constexpr (DT == UQ_BF16) {
-                const uint32_t v = __ldg((const unsigned short *)(g + k)) << (8 * (k & 2));
-                if (k < 4) w[0] |= v; else if (k < 8) w[1] |= v; else if (k < 12) w[2] |= v; else w[3] |= v;
-            } else {
-                const uint32_t v = __ldg((const uint32_t *)(g + k));
-                if (k == 0) w[0] = v; else if (k == 4) w[1] = v; else if (k == 8) w[2] = v; else w[3] = v;
+    if constexpr (DT == UQ_BF16) {
+        const char *first = (const char *)((uintptr_t)at & ~(uintptr_t)3);
+        if (have == 8 && first >= begin && first + 20 <= end) {
+            const uint32_t shift = ((uintptr_t)at & 2) * 8;
+            uint32_t w[5];
+#pragma unroll
+            for (int t = 0; t < 5; ++t) w[t] = __ldg((const uint32_t *)first + t);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) x.w[t] = __funnelshift_r(w[t], w[t + 1], shift);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const uint32_t lo = 2 * t < have ? __ldg((const unsigned short *)at + 2 * t) : 0u;
+                const uint32_t hi = 2 * t + 1 < have ? __ldg((const unsigned short *)at + 2 * t + 1) : 0u;
+                x.w[t] = lo | hi << 16;
             }
         }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    };
-    const uint4 zero = make_uint4(0, 0, 0, 0);
-    uint32_t w[W + 4];
-    const uint4 g0 = have > 0 ? granule(first) : zero;
-    w[0] = g0.x; w[1] = g0.y; w[2] = g0.z; w[3] = g0.w;
-    if constexpr (DT == UQ_F32) {
-        const uint4 g1 = have > 0 && off + 4 * have > 16 ? granule(first + 16) : zero;
-        w[4] = g1.x; w[5] = g1.y; w[6] = g1.z; w[7] = g1.w;
-    }
-    // the next lane's first granule; the last lane reads it itself
-    uint4 g2 = zero;
-    if (last && have > 0 && off + E * have > 4 * W) g2 = granule(first + 4 * W);
-    const uint32_t n0 = __shfl_down_sync(0xFFFFFFFFu, w[0], 1, 16), n1 = __shfl_down_sync(0xFFFFFFFFu, w[1], 1, 16);
-    const uint32_t n2 = __shfl_down_sync(0xFFFFFFFFu, w[2], 1, 16), n3 = __shfl_down_sync(0xFFFFFFFFu, w[3], 1, 16);
-    w[W] = last ? g2.x : n0; w[W + 1] = last ? g2.y : n1; w[W + 2] = last ? g2.z : n2; w[W + 3] = last ? g2.w : n3;
-    // words off / 4 .. of it, a half on if off is odd in words
+    } else {
 #pragma unroll
-    for (int t = 0; t < W + 2; ++t) w[t] = off & 8 ? w[t + 2] : w[t];
-#pragma unroll
-    for (int t = 0; t < W + 1; ++t) w[t] = off & 4 ? w[t + 1] : w[t];
-#pragma unroll
-    for (int t = 0; t < W; ++t) x.w[t] = DT == UQ_BF16 && (off & 2) ? __funnelshift_r(w[t], w[t + 1], 16) : w[t];
-    if (have < 8) {
-#pragma unroll
-        for (int t = 0; t < W; ++t) {
-            if constexpr (DT == UQ_BF16) x.w[t] = 2 * t + 1 < have ? x.w[t] : 2 * t < have ? x.w[t] & 0xFFFFu : 0u;
-            else x.w[t] = t < have ? x.w[t] : 0u;
-        }
+        for (int t = 0; t < 8; ++t) x.w[t] = t < have ? __ldg((const uint32_t *)at + t) : 0u;
     }
 }
 
@@ -162,8 +136,7 @@ __global__ void __launch_bounds__(kQThreads, SR ? 3 : DT == UQ_BF16 && WIDE ? 5 
                 v[k].w[0] = a.x; v[k].w[1] = a.y; v[k].w[2] = a.z; v[k].w[3] = a.w;
                 if constexpr (DT == UQ_F32) { v[k].w[4] = b.x; v[k].w[5] = b.y; v[k].w[6] = b.z; v[k].w[7] = b.w; }
             } else {
-                load_cut<DT>((const char *)x + ((r0 + r) * ld + c0) * E, (const char *)x, end, chunk, r < rows_here ? have : 0,
-                             chunk == 15 || chunk * 8 + 8 >= cols_here, v[k]);
+                load_cut<DT>((const char *)x + ((r0 + r) * ld + c0 + chunk * 8) * E, (const char *)x, end, r < rows_here ? have : 0, v[k]);
             }
         }
 #pragma unroll
