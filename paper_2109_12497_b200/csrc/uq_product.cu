@@ -21,7 +21,7 @@ struct ProductArgs {
     void *out;
     int64_t add_ld, ld;
     uint32_t *status;
-    int32_t split;                                         // CTAs (of one cluster) that share a tile's columns
+    int32_t split;                                         // CTAs (of one cluster) that share a tile's columns: 1, 2, 4 or 8
 };
 
 constexpr int kRows = 128;                                 // of b per tile
@@ -104,6 +104,38 @@ template <int NT> struct ProductShape {
     static constexpr int kColumns = NT + kStages * kScaleColumns <= 128 ? 128 : 256;
     static constexpr int kSmem = kStages * kStageBytes + 1024 + 256;
 };
+
+// Adds up columns c0 .. c1 - 1 of a tile's sums from the R CTAs of a cluster, in their order: four neighbouring rows of b per thread
+// and piece, the loads of U pieces from all CTAs in flight together.
+template <int DT, int U, int R, int THREADS>
+__device__ __forceinline__ void join_sums(const ProductArgs &p, uint32_t data, int c0, int c1, int64_t m0, int64_t n0)
+{
+    const int pieces = (c1 - c0) * (kRows / 4);
+    for (int e = threadIdx.x; e < pieces; e += U * THREADS) {
+        float4 w[U][R];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (e + u * THREADS < pieces) {
+                    const int i = e + u * THREADS;
+                    w[u][r] = cluster_load4(cluster_address(data + ((c0 + i / (kRows / 4)) * kRows + i % (kRows / 4) * 4) * 4, r));
+                }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = e + u * THREADS, c = c0 + i / (kRows / 4), l = i % (kRows / 4) * 4;
+            if (i >= pieces) break;
+            float4 v = w[u][0];
+#pragma unroll
+            for (int r = 1; r < R; ++r) { v.x += w[u][r].x; v.y += w[u][r].y; v.z += w[u][r].z; v.w += w[u][r].w; }
+            const int64_t left = p.n - n0 - l;
+            if (left > 0) store_result<DT>(p, m0 + c, n0 + l, v.x);
+            if (left > 1) store_result<DT>(p, m0 + c, n0 + l + 1, v.y);
+            if (left > 2) store_result<DT>(p, m0 + c, n0 + l + 2, v.z);
+            if (left > 3) store_result<DT>(p, m0 + c, n0 + l + 3, v.w);
+        }
+    }
+}
 
 // A tile of 128 rows of b and NT of a.  With split > 1 the CTAs of a cluster take a share of the columns each, put their sums
 // into shared memory, and each adds up a share of the tile in the CTAs' order.
@@ -227,25 +259,10 @@ __global__ void __launch_bounds__(ProductShape<NT>::kThreads) product_kernel(con
     }
     if (p.split > 1) {
         cluster_sync();
-        // Four neighbouring rows of b per thread, from all CTAs in their order; the loads of several columns in flight together.
-        const int c0 = NT * (int)rank / p.split, c1 = NT * ((int)rank + 1) / p.split;
-        for (int e = tid; e < (c1 - c0) * (kRows / 4); e += S::kThreads) {
-            const int c = c0 + e / (kRows / 4), l = e % (kRows / 4) * 4;
-            if (m0 + c >= p.m) continue;
-            float4 w[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r)
-                if (r < p.split) w[r] = cluster_load4(cluster_address(data + (c * kRows + l) * 4, r));
-            float4 v = w[0];
-#pragma unroll
-            for (int r = 1; r < 8; ++r)
-                if (r < p.split) { v.x += w[r].x; v.y += w[r].y; v.z += w[r].z; v.w += w[r].w; }
-            const int64_t left = p.n - n0 - l;
-            if (left > 0) store_result<DT>(p, m0 + c, n0 + l, v.x);
-            if (left > 1) store_result<DT>(p, m0 + c, n0 + l + 1, v.y);
-            if (left > 2) store_result<DT>(p, m0 + c, n0 + l + 2, v.z);
-            if (left > 3) store_result<DT>(p, m0 + c, n0 + l + 3, v.w);
-        }
+        const int c0 = NT * (int)rank / p.split, c1 = min(NT * ((int)rank + 1) / p.split, (int)min((int64_t)NT, p.m - m0));
+        if (p.split == 2) join_sums<DT, 4, 2, S::kThreads>(p, data, c0, c1, m0, n0);
+        else if (p.split == 4) join_sums<DT, 2, 4, S::kThreads>(p, data, c0, c1, m0, n0);
+        else join_sums<DT, 1, 8, S::kThreads>(p, data, c0, c1, m0, n0);
         cluster_sync();                                    // the others may still be reading here
     }
 }
@@ -489,17 +506,18 @@ template <int NT, int DT> cudaError_t launch_pairs(const uq_mx &a, const uq_mx &
     return cudaGetLastError();
 }
 
-// CTAs that share a tile's columns, from measured costs in microseconds: a stage takes 0.22 + 0.0018 NT of one CTA on an SM (two on
-// an SM share it), joining the sums of s CTAs 1.6 + 0.035 NT + 0.2 s.
-// 4 x 4096 x 4096: 5.3 alone, 4.5 by four; 64 x 8192 x 8192: 13.3 and 11.1;
-// 512 x 4096 x 4096, which has an SM for each tile as it is: 8.0 and, by two, 12.9.
+// CTAs that share a tile's columns, from measured costs in microseconds: a stage takes 0.2 + 0.0014 NT of one CTA on an SM (two on
+// an SM share it), joining the sums 1.3 + 0.014 NT, and 0.015 NT more where clusters share SMs.  4 x 4096 x 4096: 5.5 alone, 4.4 by
+// four; 182 x 836 x 7433: 14.7 and, by eight, 7.7; 128 x 8192 x 8192: 16.2 and, by two, 13.8; 512 x 4096 x 4096, which has an SM for
+// each tile as it is: 7.3 and, by two, 11.1.
 int best_split(int nt, int64_t tiles, int64_t stages)
 {
     int best = 1;
     double least = 1e30;
     for (int s = 1; s <= 8 && s <= stages && (s == 1 || tiles * s <= 296); s *= 2) {
         const double load = tiles * s > 148 ? (double)(tiles * s) / 148.0 : 1.0;
-        const double t = load * (double)((stages + s - 1) / s) * (0.22 + 0.0018 * nt) + (s > 1 ? 1.6 + 0.035 * nt + 0.2 * s : 0.0);
+        const double join = s > 1 ? 1.3 + 0.014 * nt + (tiles * s > 148 ? 0.015 * nt : 0.0) : 0.0;
+        const double t = load * (double)((stages + s - 1) / s) * (0.2 + 0.0014 * nt) + join;
         if (t < least) { least = t; best = s; }
     }
     return best;
