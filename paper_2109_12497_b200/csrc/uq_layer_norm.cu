@@ -12,8 +12,8 @@
 // lies beside the row (but inside the matrix) included, and a row keeps its offset from 16 bytes there.  Which elements a
 // thread holds depends on that offset: neighbours in 16-byte accesses, or elements that are 32 apart, so that a warp's scalar
 // accesses are contiguous.
-// Measured at 16384 x 8192: forward bf16 85 us (6.3 TB/s), binary32 186 us (5.8), backward bf16 161 us (5.0), binary32 260 us (6.2); with
-// rows that start anywhere (8191 columns, bf16) 147 and 269 us.
+// Measured at 16384 x 8192: forward bf16 85 us (6.3 TB/s), binary32 186 us (5.8), backward bf16 157 us (5.1), binary32 275 us (5.9); with
+// rows that start anywhere (8191 columns, bf16) 147 and 259 us; backward at 8192 x 16384 bf16 239 us (3.4), binary32 363 us (4.4).
 #include "uq_mx.cuh"
 
 namespace uq {
@@ -22,7 +22,7 @@ namespace {
 constexpr int kLnThreads = 256;                            // of the kernels for any length
 constexpr int kRing = 3;                                   // rows in shared memory
 constexpr int64_t kLnRegisterCols = 16384;                 // forward: longest row that is kept in registers
-constexpr int64_t kLnBackwardCols = 8192;                  // backward: longest row whose sums over the rows are
+constexpr int64_t kLnBackwardCols = 16384;                 // backward: longest row whose sums over the rows are (two CTAs above 8192)
 
 // How a thread's eight elements of a piece lie in the row: in 16-byte accesses (kWide: pieces that are whole or empty; kFull: none
 // is empty, so no branch is left in a row); 32 apart; neighbours, taken element by element.
@@ -231,6 +231,28 @@ template <int TPR> __device__ __forceinline__ float2 row_sums(float2 v, float2 *
             const float4 q = *(const float4 *)(scratch + w);
             v = (v + make_float2(q.x, q.y)) + make_float2(q.z, q.w);
         }
+    }
+    return v;
+}
+
+// Two sums at once over the same threads of both CTAs of a cluster: every warp leaves its sums in both.  The cluster's barrier
+// stands in for the CTA's.
+template <int TPR> __device__ __forceinline__ float2 pair_sums(float2 v, float2 *scratch, uint32_t rank)
+{
+    constexpr int W = TPR / 32;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = v + make_float2(__shfl_xor_sync(0xFFFFFFFFu, v.x, o), __shfl_xor_sync(0xFFFFFFFFu, v.y, o));
+    if ((threadIdx.x & 31) < 2) {
+        const uint32_t at = cluster_address(smem_address(scratch + rank * W + (threadIdx.x >> 5)), threadIdx.x & 31);
+        asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(at), "f"(v.x), "f"(v.y) : "memory");
+    }
+    __syncwarp();
+    cluster_sync();
+    v = both(0.0f);
+#pragma unroll
+    for (int w = 0; w < 2 * W; w += 2) {
+        const float4 q = *(const float4 *)(scratch + w);
+        v = (v + make_float2(q.x, q.y)) + make_float2(q.z, q.w);
     }
     return v;
 }
@@ -464,24 +486,34 @@ struct NormBackwardArgs {
     int64_t rows, cols, dy_ld, x_ld, dx_ld;
 };
 
+// Columns of the first CTA of two that share a row.
+__host__ __device__ __forceinline__ int64_t half_row(int64_t cols) { return ((cols + 1) / 2 + 7) & ~(int64_t)7; }
+
 // A CTA takes every gridDim.x-th row (TPR = 32: its four warps one each) and keeps its sums over the rows in registers, a
-// thread's columns being its own.
-template <int DT, int TPR, int NC, int MAP>
+// thread's columns being its own.  CL = 2: a cluster of two takes a row, half its columns each.
+template <int DT, int TPR, int NC, int MAP, int CL>
 __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kResident) layer_norm_backward_kernel(const NormBackwardArgs p)
 {
     constexpr int R = RowThreads<TPR>::kRows, T = RowThreads<TPR>::kThreads, PE = kPiece<DT, false>, NP = NC * 8 / PE;
-    __shared__ __align__(16) float2 scratch[2][TPR / 32];
+    __shared__ __align__(16) float2 scratch[2][CL * TPR / 32];
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_prologue();
-    const int t = threadIdx.x % TPR, part = threadIdx.x / TPR, cols = (int)p.cols;
-    const int slot = slot_bytes(p.cols, Elem<DT>::BYTES);
+    constexpr int E = Elem<DT>::BYTES;
+    const uint32_t rank = CL > 1 ? cluster_rank() : 0;
+    const int t = threadIdx.x % TPR, part = threadIdx.x / TPR;
+    // this CTA's columns, as a matrix of their own
+    const int64_t half = CL > 1 ? half_row(p.cols) : p.cols, col0 = rank * half;
+    const int cols = (int)min(half, p.cols - col0);
+    const char *x = (const char *)p.x + col0 * E, *dy = (const char *)p.dy + col0 * E;
+    const float *weight = p.gamma == nullptr ? nullptr : p.gamma + col0;
+    const int slot = slot_bytes(half, E);
     unsigned char *mine = ring + part * kRing * 2 * slot;
-    const int64_t first = (int64_t)blockIdx.x * R + part, step = (int64_t)gridDim.x * R;
+    const int64_t first = (int64_t)(blockIdx.x / CL) * R + part, step = (int64_t)(gridDim.x / CL) * R;
 #pragma unroll
     for (int i = 0; i < kRing; ++i) {
         if (first + i * step < p.rows) {
-            fetch<DT, TPR, MAP>(mine + 2 * i * slot, p.x, first + i * step, p.rows, p.cols, p.x_ld, t);
-            fetch<DT, TPR, MAP>(mine + (2 * i + 1) * slot, p.dy, first + i * step, p.rows, p.cols, p.dy_ld, t);
+            fetch<DT, TPR, MAP>(mine + 2 * i * slot, x, first + i * step, p.rows, cols, p.x_ld, t);
+            fetch<DT, TPR, MAP>(mine + (2 * i + 1) * slot, dy, first + i * step, p.rows, cols, p.dy_ld, t);
         }
         fetch_commit();
     }
@@ -492,14 +524,16 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         float w[PE];
 #pragma unroll
         for (int k = 0; k < PE; ++k) w[k] = 1.0f;
-        if (p.gamma != nullptr) load_weights<MAP, PE>(p.gamma, piece_at<TPR, MAP, PE>(i, t), p.cols, ((uintptr_t)p.gamma & 15) == 0, w);
+        if (weight != nullptr) load_weights<MAP, PE>(weight, piece_at<TPR, MAP, PE>(i, t), cols, ((uintptr_t)weight & 15) == 0, w);
         to_pairs<PE>(w, gamma[i]);
 #pragma unroll
         for (int k = 0; k < PE / 2; ++k) dg[i][k] = db[i][k] = both(0.0f);
     }
-    char *dxr = (char *)p.dx + first * p.dx_ld * Elem<DT>::BYTES;
+    char *dxr = (char *)p.dx + (first * p.dx_ld + col0) * E;
     fetch_wait<kRing - 1>();
-    if constexpr (TPR > 32) __syncthreads(); else __syncwarp();
+    if constexpr (CL > 1) cluster_sync();                  // (and the other CTA is there to be written to)
+    else if constexpr (TPR > 32) __syncthreads();
+    else __syncwarp();
     int s = 0, turn = 0;
     float next_mean = first < p.rows ? __ldg(p.mean + first) : 0.0f, next_rstd = first < p.rows ? __ldg(p.rstd + first) : 0.0f;
     for (int64_t row = first; row < p.rows; row += step, turn ^= 1, dxr += step * p.dx_ld * Elem<DT>::BYTES) {
@@ -508,8 +542,8 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
             next_mean = __ldg(p.mean + row + step);
             next_rstd = __ldg(p.rstd + row + step);
         }
-        const unsigned char *xr = mine + 2 * s * slot + (is_wide(MAP) ? 0 : ((uintptr_t)p.x + row * p.x_ld * Elem<DT>::BYTES) & 15);
-        const unsigned char *dr = mine + (2 * s + 1) * slot + (is_wide(MAP) ? 0 : ((uintptr_t)p.dy + row * p.dy_ld * Elem<DT>::BYTES) & 15);
+        const unsigned char *xr = mine + 2 * s * slot + (is_wide(MAP) ? 0 : ((uintptr_t)x + row * p.x_ld * E) & 15);
+        const unsigned char *dr = mine + (2 * s + 1) * slot + (is_wide(MAP) ? 0 : ((uintptr_t)dy + row * p.dy_ld * E) & 15);
         float2 d[NP][PE / 2], xh[NP][PE / 2], sum1 = both(0.0f), sum2 = both(0.0f);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {                     // beyond the row x and dy are 0: nothing is added
@@ -533,10 +567,13 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         }
         fetch_wait<kRing - 2>();                           // the next row; the barrier shows it to all, and frees this row's slot
         if constexpr (TPR == 32) __syncwarp();
-        const float2 m = row_sums<TPR>(make_float2(sum1.x + sum1.y, sum2.x + sum2.y), scratch[turn]) * both(inv_n);
+        float2 m = make_float2(sum1.x + sum1.y, sum2.x + sum2.y);
+        if constexpr (CL > 1) m = pair_sums<TPR>(m, scratch[turn], rank);
+        else m = row_sums<TPR>(m, scratch[turn]);
+        m = m * both(inv_n);
         if (row + kRing * step < p.rows) {
-            fetch<DT, TPR, MAP>(mine + 2 * s * slot, p.x, row + kRing * step, p.rows, p.cols, p.x_ld, t);
-            fetch<DT, TPR, MAP>(mine + (2 * s + 1) * slot, p.dy, row + kRing * step, p.rows, p.cols, p.dy_ld, t);
+            fetch<DT, TPR, MAP>(mine + 2 * s * slot, x, row + kRing * step, p.rows, cols, p.x_ld, t);
+            fetch<DT, TPR, MAP>(mine + (2 * s + 1) * slot, dy, row + kRing * step, p.rows, cols, p.dy_ld, t);
         }
         fetch_commit();
         s = s + 1 == kRing ? 0 : s + 1;
@@ -554,7 +591,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
             }
         }
     }
-    float *out = p.partial + (int64_t)blockIdx.x * 2 * p.cols;
+    float *out = p.partial + (int64_t)(blockIdx.x / CL) * 2 * p.cols + col0;
     if constexpr (TPR == 32) {                             // the warps' sums, in their order
         float *sums = (float *)ring;
         __syncthreads();
@@ -587,10 +624,11 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
 #pragma unroll
             for (int k = 0; k < PE; ++k) {
                 const int c = piece_at<TPR, MAP, PE>(i, t) + k * piece_step<MAP>();
-                if (c < cols) { out[c] = g[k]; out[cols + c] = b[k]; }
+                if (c < cols) { out[c] = g[k]; out[p.cols + c] = b[k]; }
             }
         }
     }
+    if constexpr (CL > 1) cluster_sync();                  // (the other CTA may still be writing its sums here)
 }
 
 // Rows of any length: dx, each row read twice (the second time from the caches).
@@ -714,8 +752,8 @@ int backward_threads(int64_t cols) { return cols <= 512 ? 32 : cols <= 1024 ? 64
 int backward_parts(int64_t rows, int64_t cols)
 {
     if (cols > kLnBackwardCols) return (int)min((rows + 63) / 64, (int64_t)64);
-    const int threads = backward_threads(cols), fewest = threads == 32 ? 16 : 4;
-    return (int)min((rows + fewest - 1) / fewest, (int64_t)148 * (512 / (threads == 32 ? 128 : threads)));
+    const int threads = backward_threads(cols), fewest = threads == 32 ? 16 : 4, resident = 512 / (threads == 32 ? 128 : threads);
+    return (int)min((rows + fewest - 1) / fewest, (int64_t)(cols > 8192 ? 74 : 148 * resident));
 }
 
 template <int DT> bool rows_wide(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0; }
@@ -757,13 +795,30 @@ template <int DT> void launch_forward_any(const NormArgs &p, cudaStream_t st)
     else launch_k(layer_norm_long_kernel<DT>, dim3((unsigned)p.rows), dim3(kLnThreads), st, p);
 }
 
-template <int DT, int TPR, int NC> void launch_backward(const NormBackwardArgs &p, bool wide, int parts, cudaStream_t st)
+template <int DT, int TPR, int NC, int CL = 1> void launch_backward(const NormBackwardArgs &p, bool wide, int parts, cudaStream_t st)
 {
     using T = RowThreads<TPR>;
-    const size_t smem = (size_t)T::kRows * kRing * 2 * slot_bytes(p.cols, Elem<DT>::BYTES);
-    if (wide && p.cols == TPR * NC * 8) launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kFull>, parts, T::kThreads, smem, st, p);
-    else if (wide) launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kWide>, parts, T::kThreads, smem, st, p);
-    else launch_rows(layer_norm_backward_kernel<DT, TPR, NC, kStrided>, parts, T::kThreads, smem, st, p);
+    const size_t smem = (size_t)T::kRows * kRing * 2 * slot_bytes(CL > 1 ? half_row(p.cols) : p.cols, Elem<DT>::BYTES);
+    auto kernel = !wide ? layer_norm_backward_kernel<DT, TPR, NC, kStrided, CL>
+                  : p.cols == CL * TPR * NC * 8 ? layer_norm_backward_kernel<DT, TPR, NC, kFull, CL> : layer_norm_backward_kernel<DT, TPR, NC, kWide, CL>;
+    if constexpr (CL == 1) {
+        launch_rows(kernel, parts, T::kThreads, smem, st, p);
+    } else {
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(parts * CL);
+        cfg.blockDim = dim3(T::kThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[2];
+        cfg.attrs = attr;
+        cfg.numAttrs = grid_dependency_attribute(attr);
+        attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+        attr[cfg.numAttrs].val.clusterDim.x = CL;
+        attr[cfg.numAttrs].val.clusterDim.y = attr[cfg.numAttrs].val.clusterDim.z = 1;
+        ++cfg.numAttrs;
+        cudaLaunchKernelEx(&cfg, kernel, p);
+    }
 }
 
 template <int DT> void launch_backward_any(const NormBackwardArgs &p, int parts, bool sums, cudaStream_t st)
@@ -774,7 +829,8 @@ template <int DT> void launch_backward_any(const NormBackwardArgs &p, int parts,
     else if (p.cols <= 1024) launch_backward<DT, 64, 2>(p, wide, parts, st);
     else if (p.cols <= 2048) launch_backward<DT, 128, 2>(p, wide, parts, st);
     else if (p.cols <= 4096) launch_backward<DT, 256, 2>(p, wide, parts, st);
-    else if (p.cols <= kLnBackwardCols) launch_backward<DT, 512, 2>(p, wide, parts, st);
+    else if (p.cols <= 8192) launch_backward<DT, 512, 2>(p, wide, parts, st);
+    else if (p.cols <= kLnBackwardCols) launch_backward<DT, 512, 2, 2>(p, wide, parts, st);
     else {
         if (p.dx != nullptr) launch_k(layer_norm_backward_long_kernel<DT>, dim3((unsigned)p.rows), dim3(kLnThreads), st, p);
         if (sums) {

@@ -6,7 +6,7 @@
 // stores need no staging whatever out's alignment and stride.
 //
 // Few tokens are bound by reading the weights (1 x 8192 x 4096: 17.8 MB in 5.4 us with the launch, 3.3 TB/s; 16 x 16384 x 8192: 5.1
-// TB/s), large products by the tensor core and the board's power (8192^3: 193 us after a pause, 5.7 PFLOP/s; 217 us back to back).
+// TB/s), large products by the tensor core and the board's power (8192^3: 184 us after a pause, 6.0 PFLOP/s; 207 us back to back).
 #include "uq_tensor.cuh"
 #include "uq_mx.cuh"
 

@@ -76,22 +76,6 @@ __device__ __forceinline__ bool elect_lane()
 
 // ---- clusters -----------------------------------------------------------------------------------
 
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
 // An arrival at a barrier of any CTA of the cluster.  It orders nothing that this thread has written to memory (a release would
 // wait for all its stores): what it says is that tensor memory has been read.
 __device__ __forceinline__ void cluster_arrive(uint32_t bar)

@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 U = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8}                   # one rounding to the type
 EPS = 1e-5
 SIZES = [(1, 1), (1, 7), (2, 32), (3, 33), (5, 255), (4, 256), (7, 1000), (3, 1025), (2, 2048), (300, 100), (5, 5001), (2, 8200),
-         (3, 16384), (2, 40003), (1000, 24)]
+         (3, 16384), (2, 40003), (1000, 24), (9, 8201), (700, 9000), (5, 16383), (330, 12280)]
 
 
 def inputs(rows, cols, seed):
