@@ -176,12 +176,13 @@ __global__ void __launch_bounds__(ProductShape<NT>::kThreads) product_kernel(con
     const uint32_t tmem = *(volatile uint32_t *)tmem_slot;
 
     if (warp == 0) {
+        const bool one = elect_lane();
         const uint8_t *scales_b = p.scales_b + (n0 >> 7) * p.ktiles * 512, *scales_a = p.scales_a + (m0 >> 7) * p.ktiles * 512;
         for (int i = s0, s = 0, parity = 1; i < s1; ++i) {
             if (i - s0 >= ST && !barrier_wait_warp(empty + 8 * s, parity, gave_up)) break;
             const uint32_t at = data + s * S::kStageBytes, bar = full + 8 * s;
             const uint32_t scale_bytes = p.ktiles - 2 * (int64_t)i >= 2 ? 1024 : 512;
-            if (elect_lane()) {
+            if (one) {
                 barrier_expect(bar, kRows * 128 + NT * 128 + 2 * scale_bytes);
                 copy_tile(at, &map_b, i * 128, (int)n0, bar);
                 copy_tile(at + kRows * 128, &map_a, i * 128, (int)m0, bar);
@@ -193,12 +194,13 @@ __global__ void __launch_bounds__(ProductShape<NT>::kThreads) product_kernel(con
             if (++s == ST) { s = 0; parity ^= 1; }
         }
     } else if (warp == 1) {
+        const bool one = elect_lane();                     // the same for all: a commit waits for what its own thread has issued
         const uint32_t codes = (uint32_t)operand_descriptor(data), scales = (uint32_t)scales_descriptor(data + kRows * 128 + NT * 128);
         for (int i = s0, s = 0, parity = 0; i < s1; ++i) {
             if (!barrier_wait_warp(full + 8 * s, parity, gave_up)) break;
             tensor_fence_after();
             const int steps = (int)min((int64_t)4, (p.k - (int64_t)i * kStageK + 63) >> 6);
-            if (elect_lane()) {
+            if (one) {
                 multiply_stage<1, NT, kRows * 128>(tmem, codes + s * (S::kStageBytes >> 4), scales + s * (S::kStageBytes >> 4),
                                                    tmem + NT + s * S::kScaleColumns, steps, i > s0);
                 tensor_commit<1>(empty + 8 * s);
@@ -206,7 +208,7 @@ __global__ void __launch_bounds__(ProductShape<NT>::kThreads) product_kernel(con
             __syncwarp();
             if (++s == ST) { s = 0; parity ^= 1; }
         }
-        if (elect_lane()) tensor_commit<1>(done);
+        if (one) tensor_commit<1>(done);
         __syncwarp();
         int again = 0;                                     // (a wait of its own: tensor memory is given back only when nothing writes it)
         if (!barrier_wait_warp(done, 0, &again)) *gave_up = 1;
@@ -277,7 +279,7 @@ __global__ void __launch_bounds__(ProductShape<NT>::kThreads) product_kernel(con
 
 template <int NT> struct PairShape {
     static constexpr int kStageBytes = kRows * 128 + NT / 2 * 128 + 1024 + (NT + 127) / 128 * 1024;
-    static constexpr int kStages = NT == 256 ? 6 : 8;
+    static constexpr int kStages = 6;
     static constexpr int kScaleSlots = 3;                  // a slot's scales are overwritten when its multiplies are done
     static constexpr int kSlotColumns = 2 * (4 + (NT + 127) / 128 * 4);
     static constexpr int kScales = 512 - kScaleSlots * kSlotColumns;      // first column of the scales
@@ -336,6 +338,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t tmem = *(volatile uint32_t *)tmem_slot;
 
     if (warp == 0) {
+        const bool one = elect_lane();
         const uint32_t leader_full = cluster_address(full, 0);
         int use = 0, s = 0, parity = 1;                    // stages filled so far; the next one, and the parity of its release
         bool going = true;
@@ -348,7 +351,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if (!going) break;
                 const uint32_t at = data + s * S::kStageBytes, bar = leader_full + 8 * s;
                 ++use;
-                if (elect_lane()) {
+                if (one) {
                     if (rank == 0) barrier_expect(full + 8 * s, 2 * S::kStageBytes);
                     copy_tile_pair(at, &map_b, i * 128, row_b, bar);
                     copy_tile_pair(at + kRows * 128, &map_a, i * 128, row_a, bar);
@@ -361,6 +364,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             }
         }
     } else if (warp == 1 && rank == 0) {
+        const bool one = elect_lane();                     // the same for all: a commit waits for what its own thread has issued
         const uint32_t codes = (uint32_t)operand_descriptor(data), scales = (uint32_t)scales_descriptor(data + kRows * 128 + NT / 2 * 128);
         const int last_steps = (int)((p.k - (int64_t)(stages - 1) * kStageK + 63) >> 6);
         int s = 0, parity = 0, slot = 0, turn = 0;
@@ -374,7 +378,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 going = (old < 0 || barrier_wait_warp(empty + 8 * old, old_parity, gave_up)) && barrier_wait_warp(full + 8 * s, parity, gave_up);
                 if (!going) break;
                 tensor_fence_after();
-                if (elect_lane()) {
+                if (one) {
                     multiply_stage<2, NT, kRows * 128>(sums, codes + s * (S::kStageBytes >> 4), scales + s * (S::kStageBytes >> 4),
                                                        tmem + S::kScales + slot * S::kSlotColumns, i + 1 < stages ? 4 : last_steps, i > 0);
                     tensor_commit<2>(empty + 8 * s);
@@ -384,12 +388,12 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if (++slot == S::kScaleSlots) slot = 0;
                 if (++old == ST) { old = 0; old_parity ^= 1; }
             }
-            if (going && elect_lane()) tensor_commit<2>(sums_ready);
+            if (going && one) tensor_commit<2>(sums_ready);
             __syncwarp();
         }
         if (*gave_up != 0) {                               // tensor memory is given back only when nothing writes it
             int again = 0;
-            if (elect_lane()) tensor_commit<2>(drained);
+            if (one) tensor_commit<2>(drained);
             __syncwarp();
             barrier_wait_warp(drained, 0, &again);
         }
