@@ -579,6 +579,11 @@ def _matrix(t: torch.Tensor, rows: int, cols: int, dtype: torch.dtype, device: i
         raise ValueError(f"uq: {what} must be a 2-D {dtype} tensor")
     if t.shape != (rows, cols):
         raise ValueError(f"uq: {what} must be [{rows}, {cols}], not {list(t.shape)}")
+    return _rows(t, rows, cols, device, what)
+
+
+def _rows(t: torch.Tensor, rows: int, cols: int, device: int, what: str):
+    """The same for a tensor of that shape and of a type that has been looked at."""
     step, inner = t.stride()
     if (inner != 1 and cols > 1) or (step < cols and rows > 1):
         raise ValueError(f"uq: the rows of {what} must be contiguous and must not overlap")
@@ -622,7 +627,7 @@ def uq_mx_quantize(x: torch.Tensor, seed: int, rng_bits: int, q: Optional[MxMatr
     blocks along x's columns, or both.  rng_bits 0: to the nearest value; 16: stochastically, unbiased."""
     device = x.get_device()
     (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
-    px, ld = _matrix(x, rows, cols, x.dtype, device, "x")
+    px, ld = _rows(x, rows, cols, device, "x")
     rc = (_lib or lib()).uq_mx_quantize(
         px, rows, cols, ld, dtype, seed & 0xFFFFFFFFFFFFFFFF, rng_bits, None if q is None else q.ref(device),
         None if qt is None else qt.ref(device), _status(status, device), _stream_of(device))
@@ -659,7 +664,7 @@ def uq_layer_norm(x: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional
     """Layer norm over the rows of x; any of y, the statistics and the quantized y (q) may be left out."""
     device = x.get_device()
     (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
-    px, ld = _matrix(x, rows, cols, x.dtype, device, "x")
+    px, ld = _rows(x, rows, cols, device, "x")
     py, y_ld = (None, 0) if y is None else _matrix(y, rows, cols, x.dtype, device, "y")
     rc = (_lib or lib()).uq_layer_norm(
         px, rows, cols, ld, dtype, _vector(gamma, cols, device, "gamma"), _vector(beta, cols, device, "beta"), eps, py, y_ld,
@@ -680,7 +685,7 @@ def uq_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: Optional[to
     of gradients.  ``workspace``: uq_layer_norm_workspace_bytes(rows, cols) bytes."""
     device = x.get_device()
     (rows, cols), dtype = _shape(x, "x"), _dtype(x, "x")
-    px, x_ld = _matrix(x, rows, cols, x.dtype, device, "x")
+    px, x_ld = _rows(x, rows, cols, device, "x")
     pdy, dy_ld = _matrix(dy, rows, cols, x.dtype, device, "dy")
     pdx, dx_ld = (None, 0) if dx is None else _matrix(dx, rows, cols, x.dtype, device, "dx")
     grad = dgamma if dgamma is not None else dbeta
