@@ -254,9 +254,9 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(y[-4:], one)
 
 
-def test_two_backward_passes_at_once():
-    """Two streams, a workspace each."""
-    rows, cols = 300, 2500
+@pytest.mark.parametrize("rows,cols", [(300, 2500), (60, 9001)])
+def test_two_backward_passes_at_once(rows, cols):
+    """Two streams, a workspace each; rows by a CTA and by a cluster of two."""
     runs = []
     for k in range(2):
         x, gamma, _, dy = inputs(rows, cols, 20 + k)

@@ -318,6 +318,33 @@ def test_on_another_stream_and_in_a_graph():
     assert torch.equal(out[scaled], 2 * want[scaled])
 
 
+def test_graphs_of_every_form_of_the_product():
+    """A tile each, tiles shared by a cluster, pairs of CTAs: captured, then replayed one after the other and on another stream."""
+    graphs = []
+    for m, n, k in ((512, 4096, 512), (1, 4096, 4096), (182, 836, 7433), (2100, 2200, 700)):
+        (a, va), (b, vb) = random_mx(m, k, m, 127, 128), random_mx(n, k, n, 127, 128)
+        out, add = torch.zeros(m, n, device="cuda"), torch.ones(m, n, device="cuda")
+        B.uq_mx_product(a, b, out, add, None)
+        torch.cuda.synchronize()
+        want = torch.from_numpy(va @ vb.T + 1).float().cuda()
+        assert torch.equal(out, want)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.uq_mx_product(a, b, out, add, None)
+        graphs.append((graph, out, want, a, b, add))
+    side = torch.cuda.Stream()
+    for stream in (torch.cuda.current_stream(), side):
+        for g in graphs:
+            g[1].zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            for g in graphs + graphs[::-1]:
+                g[0].replay()
+        torch.cuda.synchronize()
+        for g in graphs:
+            assert torch.equal(g[1], g[2])
+
+
 def test_two_streams_at_once():
     """Products of several shapes on two streams at the same time."""
     jobs = [(m, n, k, random_mx(m, k, m, 127, 128), random_mx(n, k, n, 127, 128)) for m, n, k in
