@@ -748,12 +748,17 @@ __global__ void __launch_bounds__(512) weight_gradient_kernel(const float *__res
 // Threads per row of the backward pass.
 int backward_threads(int64_t cols) { return cols <= 512 ? 32 : cols <= 1024 ? 64 : cols <= 2048 ? 128 : cols <= 4096 ? 256 : 512; }
 
-// CTAs of the backward pass, each of which leaves a part: enough to fill the GPU, and four rows for each CTA or each of its warps.
+// CTAs of the backward pass (clusters above 8192 columns), each of which leaves a part; never fewer for more rows.  A row each (for
+// a warp of it, up to 512 columns) while every SM gets one at most; then two rows, up to 400 parts, where rows are short (777 x 1025
+// binary32 by 1, 2 and 4 rows a CTA: 9.0, 8.4, 10.1 us; 4 x 8000: 8.9, 10.8, 14.7), then four: the parts have to be added up (2000 x
+// 700: 13.4, 15.0, 11.4; 600 x 4096 bf16: 17.5, 17.6, 16.3).
 int backward_parts(int64_t rows, int64_t cols)
 {
     if (cols > kLnBackwardCols) return (int)min((rows + 63) / 64, (int64_t)64);
-    const int threads = backward_threads(cols), fewest = threads == 32 ? 16 : 4, resident = 512 / (threads == 32 ? 128 : threads);
-    return (int)min((rows + fewest - 1) / fewest, (int64_t)(cols > 8192 ? 74 : 148 * resident));
+    const int threads = backward_threads(cols), at_once = threads == 32 ? 4 : 1, resident = 512 / (threads == 32 ? 128 : threads);
+    const int64_t turns = (rows + at_once - 1) / at_once, most = cols > 8192 ? 74 : 148 * resident;
+    const int64_t by_two = cols <= 2048 ? min((turns + 1) / 2, (int64_t)400) : 0;
+    return (int)min(most, max(min(turns, (int64_t)148), max(by_two, (turns + 3) / 4)));
 }
 
 template <int DT> bool rows_wide(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0; }

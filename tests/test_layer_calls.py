@@ -27,6 +27,9 @@ def test_sizes(lib):
     assert lib.uq_mx_scale_bytes(-1, 5) == 0 and lib.uq_mx_scale_bytes(1 << 31, 5) == 0
     assert lib.uq_layer_norm_workspace_bytes(-1, 5) == 0 and lib.uq_layer_norm_workspace_bytes(0, 5) == 0
     assert lib.uq_layer_norm_workspace_bytes(1, 5) >= 2 * 5 * 4
+    for cols in (100, 1000, 2000, 4000, 8000, 12000, 20000):
+        sizes = [lib.uq_layer_norm_workspace_bytes(rows, cols) for rows in range(1, 5000, 7)]
+        assert sizes == sorted(sizes)                        # a workspace for many rows does for fewer
     last = 0
     for rows in (1, 10, 100, 1000, 10 ** 6):                 # more rows never need less, and at most some megabytes for 1000 columns
         n = lib.uq_layer_norm_workspace_bytes(rows, 1000)
