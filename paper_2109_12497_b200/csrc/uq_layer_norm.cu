@@ -21,6 +21,7 @@ namespace {
 
 constexpr int kLnThreads = 256;                            // of the kernels for any length
 constexpr int kRing = 3;                                   // rows in shared memory
+constexpr size_t kLnScratchBytes = 512;                    // the most that a kernel has in shared memory beside the ring
 constexpr int64_t kLnRegisterCols = 16384;                 // forward: longest row that is kept in registers
 constexpr int64_t kLnBackwardCols = 16384;                 // backward: longest row whose sums over the rows are (two CTAs above 8192)
 
@@ -327,6 +328,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
 {
     constexpr int R = RowThreads<TPR>::kRows, PE = kPiece<DT, Q>, NP = NC * 8 / PE;
     __shared__ __align__(16) float scratch[2][TPR / 32];
+    static_assert(sizeof(scratch) <= kLnScratchBytes, "counted in launch_rows");
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_prologue();
     const int t = threadIdx.x % TPR, cols = (int)p.cols;
@@ -496,6 +498,7 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
 {
     constexpr int R = RowThreads<TPR>::kRows, T = RowThreads<TPR>::kThreads, PE = kPiece<DT, false>, NP = NC * 8 / PE;
     __shared__ __align__(16) float2 scratch[2][CL * TPR / 32];
+    static_assert(sizeof(scratch) <= kLnScratchBytes, "counted in launch_rows");
     extern __shared__ __align__(16) unsigned char ring[];
     grid_dependency_prologue();
     constexpr int E = Elem<DT>::BYTES;
@@ -763,9 +766,10 @@ int backward_parts(int64_t rows, int64_t cols)
 
 template <int DT> bool rows_wide(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0; }
 
+// A kernel has 48 KiB, its own arrays included, without asking for more.
 template <typename K, typename A> void launch_rows(K *kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, const A &args)
 {
-    if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (smem + kLnScratchBytes > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     launch_k_smem(kernel, dim3((unsigned)grid), dim3(threads), smem, st, args);
 }
 
