@@ -43,7 +43,7 @@ template <int TPR, int MAP, int PE> __device__ __forceinline__ int piece_at(int 
 template <int MAP> __device__ __forceinline__ int piece_step() { return MAP == kStrided ? 32 : 1; }
 
 // Bytes of a ring's slot: a row and the rest of its first and last granule.
-__host__ __device__ __forceinline__ int slot_bytes(int64_t cols, int bytes) { return (int)((cols * bytes + 15) / 16 * 16 + 16); }
+__host__ __device__ __forceinline__ constexpr int slot_bytes(int64_t cols, int bytes) { return (int)((cols * bytes + 15) / 16 * 16 + 16); }
 
 // Starts the copy of row `row` into a slot, by `threads` threads.  A granule that reaches out of the matrix is copied element by
 // element (the first of the first row, the last of the last row).
@@ -766,10 +766,17 @@ int backward_parts(int64_t rows, int64_t cols)
 
 template <int DT> bool rows_wide(const void *p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0; }
 
-// A kernel has 48 KiB, its own arrays included, without asking for more.
-template <typename K, typename A> void launch_rows(K *kernel, int64_t grid, int threads, size_t smem, cudaStream_t st, const A &args)
+// A kernel has 48 KiB of shared memory, its own arrays included, without asking for more.  What is asked for belongs to the kernel
+// and not to the call: every call asks for the same, `most`, or a host thread with shorter rows would take away what another one
+// is about to launch with.
+template <typename K> void ask_for_rows(K *kernel, size_t smem, size_t most)
 {
-    if (smem + kLnScratchBytes > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (smem + kLnScratchBytes > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
+template <typename K, typename A>
+void launch_rows(K *kernel, int64_t grid, int threads, size_t smem, size_t most, cudaStream_t st, const A &args)
+{
+    ask_for_rows(kernel, smem, most);
     launch_k_smem(kernel, dim3((unsigned)grid), dim3(threads), smem, st, args);
 }
 
@@ -778,15 +785,16 @@ template <int DT, int TPR, int NC> void launch_forward(const NormArgs &p, bool w
     using T = RowThreads<TPR>;
     const int64_t grid = min((p.rows + T::kRows - 1) / T::kRows, (int64_t)148 * T::kResident);
     const size_t smem = (size_t)T::kRows * kRing * slot_bytes(p.cols, Elem<DT>::BYTES);
+    constexpr size_t most = (size_t)T::kRows * kRing * slot_bytes(TPR * NC * 8, Elem<DT>::BYTES);
     const bool full = p.cols == TPR * NC * 8;
     if (p.q.codes != nullptr) {
-        if (!wide) launch_rows(layer_norm_kernel<DT, TPR, NC, kChunk, true>, grid, T::kThreads, smem, st, p);
-        else if (full) launch_rows(layer_norm_kernel<DT, TPR, NC, kFull, true>, grid, T::kThreads, smem, st, p);
-        else launch_rows(layer_norm_kernel<DT, TPR, NC, kWide, true>, grid, T::kThreads, smem, st, p);
+        if (!wide) launch_rows(layer_norm_kernel<DT, TPR, NC, kChunk, true>, grid, T::kThreads, smem, most, st, p);
+        else if (full) launch_rows(layer_norm_kernel<DT, TPR, NC, kFull, true>, grid, T::kThreads, smem, most, st, p);
+        else launch_rows(layer_norm_kernel<DT, TPR, NC, kWide, true>, grid, T::kThreads, smem, most, st, p);
     } else {
-        if (!wide) launch_rows(layer_norm_kernel<DT, TPR, NC, kStrided, false>, grid, T::kThreads, smem, st, p);
-        else if (full) launch_rows(layer_norm_kernel<DT, TPR, NC, kFull, false>, grid, T::kThreads, smem, st, p);
-        else launch_rows(layer_norm_kernel<DT, TPR, NC, kWide, false>, grid, T::kThreads, smem, st, p);
+        if (!wide) launch_rows(layer_norm_kernel<DT, TPR, NC, kStrided, false>, grid, T::kThreads, smem, most, st, p);
+        else if (full) launch_rows(layer_norm_kernel<DT, TPR, NC, kFull, false>, grid, T::kThreads, smem, most, st, p);
+        else launch_rows(layer_norm_kernel<DT, TPR, NC, kWide, false>, grid, T::kThreads, smem, most, st, p);
     }
 }
 
@@ -808,12 +816,13 @@ template <int DT, int TPR, int NC, int CL = 1> void launch_backward(const NormBa
 {
     using T = RowThreads<TPR>;
     const size_t smem = (size_t)T::kRows * kRing * 2 * slot_bytes(CL > 1 ? half_row(p.cols) : p.cols, Elem<DT>::BYTES);
+    constexpr size_t most = (size_t)T::kRows * kRing * 2 * slot_bytes(TPR * NC * 8, Elem<DT>::BYTES);
     auto kernel = !wide ? layer_norm_backward_kernel<DT, TPR, NC, kStrided, CL>
                   : p.cols == CL * TPR * NC * 8 ? layer_norm_backward_kernel<DT, TPR, NC, kFull, CL> : layer_norm_backward_kernel<DT, TPR, NC, kWide, CL>;
     if constexpr (CL == 1) {
-        launch_rows(kernel, parts, T::kThreads, smem, st, p);
+        launch_rows(kernel, parts, T::kThreads, smem, most, st, p);
     } else {
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        ask_for_rows(kernel, smem, most);
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(parts * CL);
         cfg.blockDim = dim3(T::kThreads);
