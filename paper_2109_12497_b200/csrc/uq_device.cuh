@@ -128,8 +128,8 @@ __device__ __forceinline__ uint2 ld_coherent64(const void *p)
     return v;
 }
 
-// The CTAs of a thread-block cluster: this one's number, a barrier of all their threads (converged warps), and the address in the
-// cluster of the same place in another one's shared memory.
+// The CTAs of a thread-block cluster: this one's number, a barrier of all their threads (its .aligned form wants a warp's lanes
+// together, so they meet first), and the address in the cluster of the same place in another one's shared memory.
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
@@ -138,6 +138,7 @@ __device__ __forceinline__ uint32_t cluster_rank()
 }
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t cluster_address(uint32_t addr, uint32_t rank)

@@ -247,7 +247,6 @@ template <int TPR> __device__ __forceinline__ float2 pair_sums(float2 v, float2 
         const uint32_t at = cluster_address(smem_address(scratch + rank * W + (threadIdx.x >> 5)), threadIdx.x & 31);
         asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" :: "r"(at), "f"(v.x), "f"(v.y) : "memory");
     }
-    __syncwarp();
     cluster_sync();
     v = both(0.0f);
 #pragma unroll

@@ -66,8 +66,17 @@ __device__ __forceinline__ uint32_t ld_acquire(const uint32_t *p)
     return v;
 }
 
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// (.aligned: a warp's lanes together)
+__device__ __forceinline__ void cluster_arrive()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 
 // A double of CTA `rank`'s shared memory, at the place of `p` in mine.
 __device__ __forceinline__ double ld_cluster(const double *p, uint32_t rank)
@@ -207,7 +216,6 @@ small_step_kernel(const __grid_constant__ SmallParams p)
     float W;
     if (CLUSTER) {
         norms(0, 1u);
-        __syncwarp();
         cluster_arrive();
         cluster_wait();
         W = scale_from_sums<NORM, MW>(sum_partials<NORM, MW>(0, 1, (int)gridDim.x, [&](int c, int m) { return ld_cluster(sh_part + m, c); }), M);
@@ -394,7 +402,6 @@ small_step_kernel(const __grid_constant__ SmallParams p)
     }
     }
     if (CLUSTER) {
-        __syncwarp();
         cluster_wait();
     }
 }
