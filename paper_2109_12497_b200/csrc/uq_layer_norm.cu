@@ -92,8 +92,9 @@ template <int PENDING> __device__ __forceinline__ void fetch_wait() { asm volati
 // Whether a piece holds anything of the row.
 template <int MAP> __device__ __forceinline__ bool piece_there(int at, int cols) { return MAP == kFull || at < cols; }
 
-// A piece of a row in shared memory, 0 beyond its end.
-template <int DT, int MAP, int PE> __device__ __forceinline__ void load_piece(const unsigned char *row, int at, int cols, float (&v)[PE])
+// A piece of a row in shared memory; `beyond` in the places beyond its end.
+template <int DT, int MAP, int PE>
+__device__ __forceinline__ void load_piece(const unsigned char *row, int at, int cols, float (&v)[PE], float beyond = 0.0f)
 {
     if constexpr (is_wide(MAP) && DT == UQ_BF16) {
         Elem<UQ_BF16>::unpack(*(const uint4 *)(row + at * 2), v);
@@ -115,7 +116,7 @@ template <int DT, int MAP, int PE> __device__ __forceinline__ void load_piece(co
             for (int t = 0; t < PE; ++t) v[t] = element(at + t * piece_step<MAP>());
         } else {
 #pragma unroll
-            for (int t = 0; t < PE; ++t) v[t] = at + t * piece_step<MAP>() < cols ? element(at + t * piece_step<MAP>()) : 0.0f;
+            for (int t = 0; t < PE; ++t) v[t] = at + t * piece_step<MAP>() < cols ? element(at + t * piece_step<MAP>()) : beyond;
         }
     }
 }
@@ -548,17 +549,21 @@ __global__ void __launch_bounds__(RowThreads<TPR>::kThreads, RowThreads<TPR>::kR
         const unsigned char *dr = mine + (2 * s + 1) * slot + (is_wide(MAP) ? 0 : ((uintptr_t)dy + row * p.dy_ld * E) & 15);
         float2 d[NP][PE / 2], xh[NP][PE / 2], sum1 = both(0.0f), sum2 = both(0.0f);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {                     // beyond the row x and dy are 0: nothing is added
+        for (int i = 0; i < NP; ++i) {                     // beyond the row xh and dy are 0: nothing is added
             const int at = piece_at<TPR, MAP, PE>(i, t);
             if (piece_there<MAP>(at, cols)) {
                 float w[PE];
-                load_piece<DT, MAP, PE>(xr, at, cols, w);
+                // Beyond the row mean * rstd may leave binary32 where no xh of the row does: x is the mean there, or xh is set to 0
+                // (by two CTAs 8192 x 16383 bf16 takes 344 us by the first and 305 by the second, by one 16384 x 8191 258 and 262).
+                load_piece<DT, MAP, PE>(xr, at, cols, w, CL == 1 ? mean : 0.0f);
                 to_pairs<PE>(w, xh[i]);
                 load_piece<DT, MAP, PE>(dr, at, cols, w);
                 to_pairs<PE>(w, d[i]);
 #pragma unroll
+                for (int k = 0; k < PE / 2; ++k) xh[i][k] = (xh[i][k] + both(-mean)) * both(rstd);
+                if constexpr (CL > 1) clear_beyond<MAP, PE>(at, cols, xh[i]);
+#pragma unroll
                 for (int k = 0; k < PE / 2; ++k) {
-                    xh[i][k] = (xh[i][k] + both(-mean)) * both(rstd);
                     dg[i][k] = fma2(d[i][k], xh[i][k], dg[i][k]);
                     db[i][k] = db[i][k] + d[i][k];
                     d[i][k] = d[i][k] * gamma[i][k];
