@@ -458,6 +458,20 @@ product_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     }
 }
 
+// An allocation of tensor memory waits until there is enough, and CTAs of a cluster that wait for one another's SM could wait for
+// good.  None has to wait: shared memory lets two CTAs of product_kernel onto an SM, whose columns (512 there are) fit beside each
+// other, or one of a pair, which takes all columns, with no other.
+constexpr int kSmShared = 228 * 1024, kCtaShared = 1024;   // bytes of an SM, and what each CTA takes of them beside its own
+template <int... NT> constexpr int least_smem()
+{
+    int least = kSmShared;
+    ((least = ProductShape<NT>::kSmem + kCtaShared < least ? ProductShape<NT>::kSmem + kCtaShared : least), ...);
+    return least;
+}
+template <int... NT> constexpr bool half_the_columns() { return ((ProductShape<NT>::kColumns <= 256) && ...); }
+static_assert(3 * least_smem<16, 32, 64, 128>() > kSmShared && half_the_columns<16, 32, 64, 128>(), "two CTAs per SM at most, half of the columns each");
+static_assert(PairShape<256>::kSmem + kCtaShared + least_smem<16, 32, 64, 128>() > kSmShared, "a pair's CTA has its SM to itself");
+
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                  CUtensorMapFloatOOBfill);
