@@ -507,7 +507,8 @@ int uq_mx_product(const uq_mx *a, const uq_mx *b, const void *add, int64_t add_l
  *   dx, dgamma, dbeta may each be NULL.  No rows: dgamma and dbeta are 0.
  *   workspace: uq_layer_norm_workspace_bytes(rows, cols) bytes of scratch, 16-byte aligned; calls that may overlap need
  *   one each.
- * Errors of all: UQ_ERR_BAD_ARG, UQ_ERR_UNSUPPORTED (more than 2^31 - 1 tiles of 64 x 64), UQ_ERR_WORKSPACE, UQ_ERR_CUDA.
+ * Errors of all: UQ_ERR_BAD_ARG, UQ_ERR_UNSUPPORTED (more than 2^31 - 1 tiles of 64 x 64, or of 32 x 128 where columns of
+ * binary32 are quantized), UQ_ERR_WORKSPACE, UQ_ERR_CUDA.
  */
 int uq_layer_norm(const void *x, int64_t rows, int64_t cols, int64_t ld, int dtype, const float *gamma, const float *beta,
                   float eps, void *y, int64_t y_ld, float *mean, float *rstd, const uq_mx *q, uint32_t *status, void *stream);

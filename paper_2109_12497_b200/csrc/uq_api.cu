@@ -474,7 +474,8 @@ int uq_mx_quantize(const void *x, int64_t rows, int64_t cols, int64_t ld, int dt
     if ((rng_bits != 0 && rng_bits != 16) || (q == nullptr && qt == nullptr) || !aligned(status, 4)) return UQ_ERR_BAD_ARG;
     if (q != nullptr && !mx_ok(q, rows, cols)) return UQ_ERR_BAD_ARG;
     if (qt != nullptr && !mx_ok(qt, cols, rows)) return UQ_ERR_BAD_ARG;
-    if (too_many(rows, cols)) return UQ_ERR_UNSUPPORTED;
+    if (too_many(rows, cols) || (dtype == UQ_F32 && qt != nullptr && uq::mx_ktiles(rows) * 4 * uq::mx_ktiles(cols) > 0x7FFFFFFF))
+        return UQ_ERR_UNSUPPORTED;
     if (rows == 0 || cols == 0) return UQ_OK;
     const uq_mx none = {};
     return finish(uq::launch_mx_quantize(x, rows, cols, ld, dtype, seed, rng_bits, q != nullptr ? *q : none, qt != nullptr ? *qt : none,

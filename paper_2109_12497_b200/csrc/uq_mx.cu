@@ -107,7 +107,8 @@ __global__ void __launch_bounds__(kQThreads, SR ? 3 : DT == UQ_BF16 && WIDE ? 5 
 {
     constexpr int E = Elem<DT>::BYTES, BATCH = TR == 32 ? 2 : DT == UQ_BF16 ? 8 : 4;
     extern __shared__ __align__(16) unsigned char smem[];
-    const bool along_rows = q.codes != nullptr, along_cols = qt.codes != nullptr;
+    constexpr bool COLS = DT == UQ_BF16 || TR == 32;       // (binary32 columns: always a quarter of a tile)
+    const bool along_rows = q.codes != nullptr, along_cols = COLS && qt.codes != nullptr;
     unsigned char *scales_q = smem, *scales_t = smem + 512, *tile = smem + 1024, *draws = tile + kTileBytes<DT, TR>;
     grid_dependency_prologue();
     const int64_t ktq = mx_ktiles(cols), ktt = mx_ktiles(rows);
@@ -323,8 +324,8 @@ void launch_tile(const void *x, int64_t rows, int64_t cols, int64_t ld, const Ph
 {
     const bool wide = ((uintptr_t)x & 15) == 0 && (ld * Elem<DT>::BYTES & 15) == 0 && (cols & 7) == 0;
     const int64_t tiles = mx_ktiles(cols) * mx_ktiles(rows);
-    const bool small = tiles <= kQuarterTiles || (DT == UQ_F32 && qt.codes != nullptr && 4 * tiles <= 0x7FFFFFFF);
-    const size_t tile = small ? kTileBytes<DT, 32> + (SR ? kTileBytes<UQ_BF16, 32> : 0) : kTileBytes<DT, 128> + (SR ? kTileBytes<UQ_BF16, 128> : 0);
+    const bool small = tiles <= kQuarterTiles || (DT == UQ_F32 && qt.codes != nullptr);
+    const size_t tile = small ? kTileBytes<DT, 32> + (SR ? kTileBytes<UQ_BF16, 32> : 0) : kTileBytes<UQ_BF16, 128> * (SR ? 2 : 1);
     const size_t smem = 1024 + (qt.codes != nullptr ? tile : 0);
     auto kernel = small ? (wide ? quantize_tile_kernel<DT, SR, true, 32> : quantize_tile_kernel<DT, SR, false, 32>)
                         : (wide ? quantize_tile_kernel<DT, SR, true, 128> : quantize_tile_kernel<DT, SR, false, 128>);
