@@ -42,8 +42,8 @@ template <int DT> __device__ __forceinline__ void store_result(const ProductArgs
     store1<DT>(p.out, i * p.ld + j, v);
 }
 
-// 16 rows of out (or of what is added) from row i on, in this lane's column of the 32 from j0 on; `have` of them exist.  The rows'
-// addresses are the same for a warp: they stay in uniform registers, and a lane adds its constant offset.
+// 16 rows of out (or of what is added) from row i on, in this lane's column of the 32 from j0 on; `have` of them exist.  A row's
+// address is the same for a warp; a lane adds its offset, which stays.
 template <int DT> __device__ __forceinline__ void load_column(const void *base, int64_t ld, int64_t i, int64_t j0, int lane, int have, float (&v)[16])
 {
     const char *row = (const char *)base + (i * ld + j0) * Elem<DT>::BYTES;

