@@ -500,7 +500,8 @@ int uq_mx_product(const uq_mx *a, const uq_mx *b, const void *add, int64_t add_l
  * uq_layer_norm — per row: mean = sum x / cols, var = sum (x - mean)^2 / cols, rstd = 1 / sqrt(var + eps),
  *   y = (x - mean) * rstd * gamma + beta.  dtype is the type of x and y; gamma, beta, mean, rstd are binary32; gamma and
  *   beta may be NULL (1 and 0), and any of y, mean, rstd, q.  q receives y (rounded to dtype) quantized to the nearest, as
- *   uq_mx_quantize would write it.  status (only with q): UQ_STATUS_NONFINITE.  cols >= 1.
+ *   uq_mx_quantize would write it.  status (only with q): UQ_STATUS_NONFINITE.  cols >= 1.  All is binary32: of a row whose
+ *   squares add up beyond its range (values above some 1e18) rstd is 0.
  * uq_layer_norm_backward — with xh = (x - mean) * rstd and t = dy * gamma:
  *   dx = rstd * (t - sum t / cols - xh * sum (t * xh) / cols), dgamma[c] = sum over rows of dy * xh, dbeta[c] = sum over
  *   rows of dy, binary32 sums in an order fixed by the sizes; dgamma and dbeta (grad_dtype) may lie in a worker's row of g.

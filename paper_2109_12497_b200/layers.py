@@ -3,9 +3,13 @@
 ``NormLinear`` is layer norm followed by a linear map without a bias, the products in microscaled 4-bit arithmetic.  Its
 parameters lie in one flat binary32 vector, ``[gamma | beta | weight]``, and its backward pass writes their gradients to the
 same places of one worker's row of ``g``; the step's update (``Quantizer.aggregate_decode_update``) then moves the vector.
-Activations and weights are rounded to the nearest 4-bit value; gradients stochastically, so that the weight's gradient is
-unbiased like everything that the quantizers do to it afterwards.  It holds buffers and makes the calls of the C ABI; it
-holds no arithmetic.
+
+Activations y and weights W are rounded to the nearest 4-bit value, Q; the gradient dy stochastically.  So the weight's gradient
+is unbiased for dy^T Q(y) and the input's (in front of layer norm) for dy Q(W), as the quantizers that follow are for what they
+are given; they are not for dy^T y and dy W.  Nor is the backward pass the derivative of the forward pass: that one uses y and W
+with blocks along d_in, this one the same matrices with blocks along the tokens and along d_out, which are other roundings.
+
+The class holds buffers and makes the calls of the C ABI; it holds no arithmetic.
 """
 from __future__ import annotations
 
@@ -77,8 +81,10 @@ class NormLinear:
         return self.out
 
     def infer(self, x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """The same result for any number of rows of up to ``tokens`` (new tokens in serving), in two kernels: the
-        normalised rows leave layer norm quantized."""
+        """The forward pass for any number of rows of up to ``tokens`` (new tokens in serving), in two kernels: the normalised
+        rows leave layer norm quantized.  Its binary32 sums may have another order than ``forward``'s (and another one for
+        another number of rows), and a value of y that this takes across a border gets the neighbouring code (float32, 300 x
+        4096: 4 of 12 million bytes of codes).  Without ``out`` the result is a part of the buffer that ``forward`` returns."""
         self._loaded()
         n = x.shape[0]
         if not 1 <= n <= self.tokens:
