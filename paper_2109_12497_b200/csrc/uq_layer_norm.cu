@@ -12,8 +12,10 @@
 // lies beside the row (but inside the matrix) included, and a row keeps its offset from 16 bytes there.  Which elements a
 // thread holds depends on that offset: neighbours in 16-byte accesses, or elements that are 32 apart, so that a warp's scalar
 // accesses are contiguous.
-// Measured at 16384 x 8192: forward bf16 85 us (6.3 TB/s), binary32 186 us (5.8), backward bf16 157 us (5.1), binary32 275 us (5.9); with
-// rows that start anywhere (8191 columns, bf16) 147 and 259 us; backward at 8192 x 16384 bf16 239 us (3.4), binary32 363 us (4.4).
+// Measured at 16384 x 8192: forward bf16 85 us (6.3 TB/s), binary32 188 us (5.7), quantized on the way out 127 us and 153 us (2.7 and
+// 4.0), with the result itself as well 134 and 188 us, backward bf16 158 us (5.1), binary32 254 to 275 us (5.9 to 6.3); with rows that
+// start anywhere (8191 columns) bf16 148, 207 and 259 us, binary32 188, 271 and 290; backward at 8192 x 16384 bf16 239 us (3.4),
+// binary32 363 us (4.4).
 #include "uq_mx.cuh"
 
 namespace uq {
@@ -109,8 +111,8 @@ __device__ __forceinline__ void load_piece(const unsigned char *row, int at, int
             if constexpr (DT == UQ_BF16) return __uint_as_float((uint32_t)*(const unsigned short *)(row + i * 2) << 16);
             else return *(const float *)(row + i * 4);
         };
-        // all but a row's last pieces without questions: 16384 x 8191 forward 167 -> 147 us (binary32, with half the elements to a
-        // piece, loses by the second copy of the code)
+        // all but a row's last pieces without questions: 16384 x 8191 bf16 forward 167 -> 147 us (binary32, with half the elements to a
+        // piece, loses by it)
         if (DT == UQ_BF16 && at + (PE - 1) * piece_step<MAP>() < cols) {
 #pragma unroll
             for (int t = 0; t < PE; ++t) v[t] = element(at + t * piece_step<MAP>());
@@ -756,9 +758,12 @@ __global__ void __launch_bounds__(512) weight_gradient_kernel(const float *__res
 int backward_threads(int64_t cols) { return cols <= 512 ? 32 : cols <= 1024 ? 64 : cols <= 2048 ? 128 : cols <= 4096 ? 256 : 512; }
 
 // CTAs of the backward pass (clusters above 8192 columns), each of which leaves a part; never fewer for more rows.  A row each (for
-// a warp of it, up to 512 columns) while every SM gets one at most; then two rows, up to 400 parts, where rows are short (777 x 1025
-// binary32 by 1, 2 and 4 rows a CTA: 9.0, 8.4, 10.1 us; 4 x 8000: 8.9, 10.8, 14.7), then four: the parts have to be added up (2000 x
-// 700: 13.4, 15.0, 11.4; 600 x 4096 bf16: 17.5, 17.6, 16.3).
+// a warp of it, up to 512 columns) while every SM gets one at most; then four: the parts have to be added
+// up (600 x 4096 bf16 by 1, 2 and 4 rows: 17.5, 17.6, 16.3 us; 4 x 8000: 8.9, 10.8, 14.7).  Between the two, where rows are short, two
+// rows, up to 400 parts (both passes replayed as a graph; by four rows, by two up to 400 parts, by two without a limit: 777 x 1025
+// binary32 10.0, 8.4, 8.4 us; 3200 x 500 14.4, 12.1, 12.1; 1000 x 1025 bf16 11.3, 9.4, 9.4; 1000 x 2000 bf16 17.3, 17.3, 20.4; 2000 x
+// 700 binary32 11.4, 11.5, 14.8; of 24 sizes in both types two rows gain most at 3200 x 500 bf16, 15.4, 12.3, and lose most at 600 x
+// 2000 bf16, 12.5, 15.9).
 int backward_parts(int64_t rows, int64_t cols)
 {
     if (cols > kLnBackwardCols) return (int)min((rows + 63) / 64, (int64_t)64);

@@ -5,8 +5,10 @@
 // contiguous bytes of every row of codes.  In either orientation a lane holds eight neighbours of a block and four lanes are a
 // block, whose largest magnitude two shuffles find.  Columns are read back from the tile in shared memory, bf16 values and the
 // draws (made once per eight values of a row, used in both orientations) by transposing matrix loads.
-// To the nearest it is bound by memory (16384 x 8192 bf16 along rows 57 to 60 us, 5.7 to 6.0 TB/s).  Where it draws, by arithmetic:
-// 38 instructions per value both ways, 22 of them on the integer pipe, which is 75 % busy (210 us, 2.0 TB/s; binary32 296 us).
+// To the nearest and along rows it is bound by memory (16384 x 8192 bf16 57 to 60 us, 5.7 to 6.0 TB/s, binary32 93 us, 6.5); along
+// columns it takes 68 and 144 us, both ways 100 and 163 (the floors by bytes are 53 and 94 us one way, 64 and 105 both).  Where it
+// draws, it is bound by arithmetic: 38 instructions per value both ways, 22 of them on the integer pipe, which is 75 % busy (bf16
+// along rows, along columns, both ways 131, 134, 210 us; binary32 142, 202, 292).
 #include "uq_mx.cuh"
 
 namespace uq {
@@ -72,8 +74,8 @@ template <int DT> __device__ __forceinline__ void keep_eight(unsigned char *tile
 }
 // Eight values from `at` on, whatever its alignment; `have` of them exist.  bf16: five words that the values touch (what lies beside
 // the row, but inside the matrix, included), cut where a half is over; single values at the matrix's ends and a row's end.  (Whole
-// 16-byte granules, completed by the next lane's, read memory in fewer instructions but cost 20 more on the pipe that bounds the
-// kernel: 8192 x 8191 stochastic both ways 143 us against 131, binary32 175 against 152.)
+// 16-byte granules, completed by the next lane's, read memory in fewer instructions but take longer: 8192 x 8191 stochastic both
+// ways 143 us against 131, binary32 175 against 152.)
 template <int DT> __device__ __forceinline__ void load_cut(const char *at, const char *begin, const char *end, int have, Eight<DT> &x)
 {
     if constexpr (DT == UQ_BF16) {

@@ -31,7 +31,7 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t amax_bits)
     return up > 2u ? up - 2u : 0u;
 }
 
-// 2^-e for a finite block's scale byte (0 .. 252): exponent field 254 - byte, never subnormal.
+// 2^-e for a finite block's scale byte (0 .. 253): exponent field 254 - byte, never subnormal.
 __device__ __forceinline__ float mx_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
 // 2^e.

@@ -5,8 +5,10 @@
 // tokens) its columns: few tokens then cost few columns, and a warp's 32 lanes are 32 neighbouring elements of a row of out, so
 // stores need no staging whatever out's alignment and stride.
 //
-// Few tokens are bound by reading the weights (1 x 8192 x 4096: 17.8 MB in 5.4 us with the launch, 3.3 TB/s; 16 x 16384 x 8192: 5.1
-// TB/s), large products by the tensor core and the board's power (8192^3: 184 us after a pause, 6.0 PFLOP/s; 207 us back to back).
+// Few tokens are bound by reading the weights.  From HBM, where a model's layers lie between one token and the next (a ring of
+// matrices of 400 MB, as a graph): 1 x 8192 x 4096 (17.8 MB) 6.4 us, 2.8 TB/s, 16 x 16384 x 8192 14.0 us, 5.1 TB/s, 37 x 10000 x 5010 9.8
+// us, 2.8 TB/s; the same matrix again and again, out of the L2 cache: 5.2, 8.9 and 8.2 us.  Large products are bound by the tensor
+// core and the board's power (8192^3: 184 us after a pause, 6.0 PFLOP/s; 207 to 214 us back to back).
 #include "uq_tensor.cuh"
 #include "uq_mx.cuh"
 

@@ -83,8 +83,8 @@ class NormLinear:
     def infer(self, x: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The forward pass for any number of rows of up to ``tokens`` (new tokens in serving), in two kernels: the normalised
         rows leave layer norm quantized.  Its binary32 sums may have another order than ``forward``'s (and another one for
-        another number of rows), and a value of y that this takes across a border gets the neighbouring code (float32, 300 x
-        4096: 4 of 12 million bytes of codes).  Without ``out`` the result is a part of the buffer that ``forward`` returns."""
+        another number of rows), and a value of y that this takes across a border gets the neighbouring code (float32, 20 x 300
+        x 4096: 4 of 12 million bytes of codes).  Without ``out`` the result is a part of the buffer that ``forward`` returns."""
         self._loaded()
         n = x.shape[0]
         if not 1 <= n <= self.tokens:
